@@ -266,6 +266,68 @@ int sgc_decode_step_batched_noalloc(sgc_ctx *ctx, const sgc_cache *cache, sgc_pl
                                     int32_t step, const void *dev_q, const void *dev_k, const void *dev_v,
                                     void *dev_o, float *dev_lse, void *hip_stream);
 
+/* ---- drafted decoding: several new tokens of every query at once ---------------------------------------
+ * Generation one token a step reads the cached prompts, the queries' own keys and every weight for one row a query.  Where something
+ * cheap proposes the next tokens (a small model, a look-up in the prompt), one pass checks them all: the last token that stands and the
+ * drafted tokens behind it go through the layers together, and the target's probabilities say how many of them stand
+ * (sgc_verify_drafts).  How far each query has got lives on the device: nothing waits for the host between passes, and a pass can
+ * be captured into a graph and replayed.
+ *
+ * sgc_plan_enable_drafts: host-only; call it before the plan's first suffix prefill.  Does what
+ * sgc_plan_enable_decode(plan, max_new_tokens) does (decode steps may be taken as well), and makes room for passes of up to max_rows
+ * tokens a query, 1 <= max_rows <= 16 and <= max_new_tokens.  max_new_tokens counts all tokens behind the question whose keys are in the pages at
+ * once: those that stand, and those of the pass on its way.
+ *
+ * sgc_draft_step_batched: one layer, one pass.  Query n brings dev_rows[n] tokens (dev_rows NULL: max_rows), of which token j
+ * sits at position prefix_len + suffix_len + dev_done[n] + j and sees the cached prompt, the question, the first dev_done[n] generated tokens and
+ * tokens 0 .. j of the pass.  dev_q / dev_o: [n_queries][max_rows][Hq][d], dev_k / dev_v: [n_queries][max_rows][Hkv][d], before rotation,
+ * queries in original order; dev_lse (may be NULL): [Hq][n_queries * max_rows] fp32, natural log.  The tokens' rotated keys and values go into
+ * the query's pages of this layer behind the first dev_done[n] generated ones, over whatever a refused draft left there.
+ * Counts are read on the device, and held to the pages: rows from dev_rows[n] on, and rows that would lie at or behind max_new_tokens, are left as
+ * they are, in dev_o, dev_lse and the pages alike; so are all rows of a query whose dev_done[n] is negative or dev_rows[n] below one.
+ * The pass's results go by its own arguments and the pages alone: repeated with the same counts it gives the same bits.
+ * dev_o and dev_lse may not overlap dev_q, dev_k or dev_v (SGC_EINVAL).  A value that is not finite among the pass's new tokens can turn that channel
+ * of the query's other rows of the pass into NaN.  bf16 io, head_dim 128, as decode steps.
+ * Allocates nothing once the plan is uploaded and the rotary table covers its positions (max_position); where the tables are stale
+ * the call refreshes them, except under capture (SGC_ESTATE).  Run the question's suffix prefill of every layer first (sgc_plan_upload where no query has question
+ * tokens); move the counts on when the last layer is through. */
+int sgc_plan_enable_drafts(sgc_plan *plan, int32_t max_new_tokens, int32_t max_rows);
+int sgc_draft_step_batched(sgc_ctx *ctx, const sgc_cache *cache, sgc_plan *plan, int32_t layer, const int32_t *dev_done,
+                           const int32_t *dev_rows, const void *dev_q, const void *dev_k, const void *dev_v, void *dev_o,
+                           float *dev_lse, void *hip_stream);
+
+/* sgc_token_probs: probabilities of rows of logits, p_i = exp((x_i - max x) / temperature) / sum, in fp32.  dev_logits: n_rows rows of
+ * vocab elements (logits_dtype SGC_F32 or SGC_BF16), logits_stride elements apart; dev_probs: the same, probs_stride apart.  temperature
+ * 0: one at the largest logit (the first of equal ones), zero elsewhere.  A logit of minus infinity or NaN is a token ruled out; a row
+ * that rules out all of them gets zeros; logits of plus infinity share the row equally.  Arrays need their element type's alignment only.  dev_workspace: sgc_token_probs_workspace bytes
+ * (0 for many rows), 16-byte aligned, contents of no meaning before and after.  dev_probs may not overlap dev_logits.  ctx may be NULL (it only receives the error text). */
+size_t sgc_token_probs_workspace(int64_t n_rows, int32_t vocab);
+int sgc_token_probs(sgc_ctx *ctx, int64_t n_rows, int32_t vocab, const void *dev_logits, int32_t logits_dtype, int64_t logits_stride,
+                    float temperature, float *dev_probs, int64_t probs_stride, void *dev_workspace, size_t workspace_bytes, void *hip_stream);
+
+/* sgc_verify_drafts: which drafted tokens stand, by the target's probabilities and given random numbers, and the token behind them, so that
+ * what comes out is distributed as if it had been drawn from the target's probabilities token by token.
+ *   dev_tokens [n_queries][max_rows]   what the pass was run on: the last token that stood, then the drafts
+ *   dev_rows [n_queries] or NULL       tokens of the pass per query, as for sgc_draft_step_batched (so dev_rows[n] - 1 drafts)
+ *   dev_target [n_queries][max_rows]   rows of vocab probabilities, target_stride elements apart: row j says what follows token j
+ *   dev_draft [n_queries][max_rows - 1]   rows of the drafts' probabilities, draft_stride apart: row j is what draft j + 1 was drawn from;
+ *                                      NULL: drafts are not drawn (copied from the prompt, the likeliest token), their probability is one
+ *   dev_uniform [n_queries][max_rows]  numbers in [0, 1): number j tests draft j + 1, the LAST one (max_rows - 1) draws the token behind
+ * Draft j + 1, token x, stands if those before it do and uniform * draft[j][x] < target[j][x] (in 64 bits; a token outside [0, vocab) does not stand).
+ * Behind accepted drafts the next token is drawn from the target's row, or, if a draft was refused there, from max(target - draft, 0) of that
+ * row (the target's row if that is zero everywhere): the first token at which the running sum of the weights, in 64 bits, exceeds uniform times their sum.
+ * The weights need not sum to one; a NaN weighs nothing; a row without any weight gives -1.
+ *   dev_out_tokens [n_queries][max_rows]   the accepted drafts, the token behind them, then -1
+ *   dev_accepted [n_queries]           number of accepted drafts
+ *   dev_done [n_queries] or NULL       raised by accepted + 1: the tokens of the pass whose keys stay in the pages
+ * A query with fewer than one row gets 0 accepted, -1 for every token, and keeps its dev_done.  Arrays need their element type's alignment only.
+ * dev_workspace: sgc_verify_workspace bytes, 16-byte aligned (may be 0), contents of no meaning before and after.  The outputs may not overlap the inputs.  ctx may be NULL. */
+size_t sgc_verify_workspace(int32_t n_queries, int32_t vocab);
+int sgc_verify_drafts(sgc_ctx *ctx, int32_t n_queries, int32_t max_rows, int32_t vocab, const float *dev_target, int64_t target_stride,
+                      const float *dev_draft, int64_t draft_stride, const int32_t *dev_tokens, const int32_t *dev_rows,
+                      const float *dev_uniform, int32_t *dev_out_tokens, int32_t *dev_accepted, int32_t *dev_done,
+                      void *dev_workspace, size_t workspace_bytes, void *hip_stream);
+
 /* ---- query clustering (Sec. 3.2; App. A.2; linkages of Table 3) -------------------------------
  * Agglomerative hierarchical clustering of m query (subgraph) embeddings with Euclidean distance,
  * stopped when n_clusters clusters are left ("cutting the dendrogram at a predefined number of
@@ -335,6 +397,27 @@ int sgc_project_qkv_suffix(sgc_ctx *ctx, const sgc_cache *cache, sgc_plan *plan,
                            void *hip_stream);
 int sgc_project_out(sgc_ctx *ctx, const void *dev_o, const void *dev_w_o, int32_t d_model, int64_t n_tokens,
                     void *dev_y, void *hip_stream);
+
+/* ---- projections with 8-bit weights -----------------------------------------------------------------
+ * y = x W^T for a layer's projections and the head, W in OCP e4m3 codes with a scale for each 128 x 128 of it: half the bytes to
+ * read where a pass has few rows, twice the matrix rate where it has many.  x comes in 16 or 32 bits and is quantised on the way, with a scale for
+ * each 128 of a row.  A scale is a power of two, kept as its exponent plus 127 in a byte: the smallest that brings the block's
+ * largest magnitude to 448 or below (2^0 for a block of zeros).  Codes are x / scale rounded to nearest even; what is not finite
+ * does not count for the scale and becomes NaN, and so does every y it enters.  Sums are fp32; y is rounded once, when stored.
+ *
+ * sgc_quantise_weight_fp8: dev_w [n_features][d_model] (SGC_F32 or SGC_BF16, contiguous) -> dev_codes [n_features][Kp] with
+ * Kp = d_model rounded up to 128 and zeros from d_model on, dev_exponents [ceil(n_features / 128)][Kp / 128].  Codes and exponents that come
+ * from elsewhere may be used as they are if they are laid out so.  Once per weight.
+ * sgc_project_fp8: dev_x: n_rows rows of d_model elements, x_stride elements apart, every row 16-byte aligned; dev_y: n_rows rows of
+ * n_features elements, y_stride apart, aligned to their type; nothing between or behind the rows is touched.  n_features: any; d_model: a
+ * multiple of 16.  x_dtype and y_dtype: SGC_F32 or SGC_BF16.  dev_workspace: sgc_project_fp8_workspace bytes, 16-byte aligned, contents of no meaning before and
+ * after.  dev_y may not overlap dev_x.  The order of the sums follows from the sizes: the same call gives the same bits.  ctx may be NULL (both). */
+int sgc_quantise_weight_fp8(sgc_ctx *ctx, const void *dev_w, int32_t w_dtype, int32_t n_features, int32_t d_model, void *dev_codes,
+                            void *dev_exponents, void *hip_stream);
+size_t sgc_project_fp8_workspace(int64_t n_rows, int32_t n_features, int32_t d_model);
+int sgc_project_fp8(sgc_ctx *ctx, const void *dev_x, int32_t x_dtype, int64_t x_stride, int64_t n_rows, const void *dev_codes,
+                    const void *dev_exponents, int32_t n_features, int32_t d_model, void *dev_y, int32_t y_dtype, int64_t y_stride,
+                    void *dev_workspace, size_t workspace_bytes, void *hip_stream);
 
 /* ---- kernel timing (measurement aid; no effect on results) -----------------------------------
  * With timing on, sgc_suffix_prefill_batched records HIP events on its launch stream around what it

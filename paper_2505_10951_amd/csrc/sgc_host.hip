@@ -499,13 +499,17 @@ void fill_tile_pt_off(sgc_plan *pl, const sgc_cache *c)
         t.pt_off = off[t.cluster];
         fill_first_pages(t, c->cl[t.cluster].pages);
     }
-    for (size_t i = 0; i < pl->dtiles.size(); ++i) {      // a decode tile covers the key range that starts at dtile_key0
-        Tile &t = pl->dtiles[i];
-        if (t.n_rows == 0) continue;
-        const int first = pl->dtile_key0[i] / kPageTokens;
-        t.pt_off = off[t.cluster] + first;
-        fill_first_pages(t, c->cl[t.cluster].pages, first, (t.prefix_len + kPageTokens - 1) / kPageTokens);
-    }
+    auto ranges = [&](std::vector<Tile> &list, const std::vector<int32_t> &key0) {      // such a tile covers the key range that starts at its key0
+        for (size_t i = 0; i < list.size(); ++i) {
+            Tile &t = list[i];
+            if (t.n_rows == 0) continue;
+            const int first = key0[i] / kPageTokens;
+            t.pt_off = off[t.cluster] + first;
+            fill_first_pages(t, c->cl[t.cluster].pages, first, (t.prefix_len + kPageTokens - 1) / kPageTokens);
+        }
+    };
+    ranges(pl->dtiles, pl->dtile_key0);
+    ranges(pl->ftiles, pl->ftile_key0);
     pl->tiles_generation = c->generation;
 }
 
@@ -676,8 +680,79 @@ void build_decode_tiles(sgc_plan *pl, int tile_rows)
     for (size_t sq = 0; sq < pl->sq_len.size(); ++sq) pl->dtok[sq] = {pl->sq_query[sq], pl->sq_len[sq], pl->sq_page0[sq], 0};
 }
 
+// Row tiles of passes over drafted tokens: max_rows x g rows per query, all queries of a (cluster, KV head) stacked, the cached keys of
+// every row tile split into ranges as for decode steps.  A pass has max_rows times a step's rows, and more tiles of its own to fill the
+// chip with.
+void build_draft_tiles(sgc_plan *pl, int tile_rows)
+{
+    const sgc_ctx *ctx = pl->ctx;
+    const int R = pl->draft_rows;
+    const int64_t per_query = (int64_t)R * (ctx->p.n_q_heads / ctx->p.n_kv_heads);
+    struct Unit {
+        int32_t cluster, hk;
+        int64_t rows;
+    };
+    std::vector<Unit> units;
+    std::vector<double> work;
+    int64_t row_tiles = 0, max_steps = 0;
+    for (int c = 0; c < pl->n_clusters; ++c) {
+        const int64_t rows = (pl->cl_sq_off[c + 1] - pl->cl_sq_off[c]) * per_query;
+        if (rows == 0) continue;
+        const int64_t nt = (rows + tile_rows - 1) / tile_rows;
+        row_tiles += nt * ctx->p.n_kv_heads;
+        max_steps = std::max<int64_t>(max_steps, (pl->cl_prefix_len[c] + 63) / 64);
+        for (int hk = 0; hk < ctx->p.n_kv_heads; ++hk) {
+            units.push_back({c, hk, rows});
+            work.push_back((double)nt * (pl->cl_prefix_len[c] + 64.0));
+        }
+    }
+    int S = 1;
+    if (row_tiles > 0) {
+        const int64_t full = std::min(max_steps / 8, std::max<int64_t>(512 / row_tiles, 1)), half = std::min({max_steps / 3, std::max<int64_t>(256 / row_tiles, 1), (int64_t)8});
+        S = (int)std::min<int64_t>(kDecodeMaxSplits, std::max({(int64_t)1, full, half}));
+    }
+    if (max_steps >= (1 << 24) / 64) S = 1;      // the position offset travels in 24 bits of the tile record
+    pl->draft_splits = S;
+    std::array<std::vector<std::pair<Tile, int32_t>>, kXcd> lists;
+    const auto of_xcd = deal_to_xcds(work);
+    for (int x = 0; x < kXcd; ++x)
+        for (int ui : of_xcd[x]) {
+            const Unit &u = units[ui];
+            const int P = pl->cl_prefix_len[u.cluster], steps = (P + 63) / 64;
+            for (int64_t r = 0; r < u.rows; r += tile_rows)
+                for (int sp = 0; sp < S; ++sp) {
+                    const int key0 = std::min(P, 64 * (int)((int64_t)steps * sp / S)), key1 = std::min(P, 64 * (int)((int64_t)steps * (sp + 1) / S));
+                    Tile t{};
+                    t.cluster = u.cluster;
+                    t.hk = u.hk;
+                    t.row0 = (int32_t)r;
+                    t.n_rows = (int32_t)std::min<int64_t>(tile_rows, u.rows - r);
+                    t.prefix_len = key1 - key0;
+                    t.pad = (sp << 24) | (P - t.prefix_len);
+                    t.tok_base = pl->cl_sq_off[u.cluster] * R;
+                    t.sq_hi = -1;
+                    t.n_q = kTileQueries + 1;             // row bookkeeping from the table
+                    lists[x].push_back({t, key0});
+                }
+        }
+    size_t slots = 0;
+    for (auto &l : lists) slots = std::max(slots, l.size());
+    pl->ftiles.assign(slots * kXcd, Tile{});
+    pl->ftile_key0.assign(slots * kXcd, 0);
+    for (int x = 0; x < kXcd; ++x)
+        for (size_t k = 0; k < lists[x].size(); ++k) {
+            pl->ftiles[k * kXcd + x] = lists[x][k].first;
+            pl->ftile_key0[k * kXcd + x] = lists[x][k].second;
+        }
+    pl->ftok.resize(pl->sq_len.size() * R);
+    for (size_t sq = 0; sq < pl->sq_len.size(); ++sq)
+        for (int j = 0; j < R; ++j) pl->ftok[sq * R + j] = {pl->sq_query[sq] * R + j, pl->sq_len[sq], pl->sq_page0[sq], pl->sq_query[sq] << 5 | j};
+}
+
 void plan_free_device(sgc_plan *pl)
 {
+    dev_release(pl->ctx, pl->draft_scratch, pl->last_stream);
+    pl->draft_scratch = sgc_dev_block{};
     dev_release(pl->ctx, pl->dec_scratch, pl->last_stream);
     pl->dec_scratch = sgc_dev_block{};
     pl->dec_counters_cleared = 0;
@@ -699,6 +774,20 @@ void plan_free_device(sgc_plan *pl)
 }
 
 }  // namespace
+
+namespace sgc {
+
+int report(sgc_ctx *ctx, int code, const char *fmt, ...)
+{
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof(buf), fmt, ap);
+    va_end(ap);
+    return fail(ctx, code, "%s", buf);
+}
+
+}  // namespace sgc
 
 extern "C" {
 
@@ -1287,6 +1376,17 @@ static ExpandArgs plan_expand_args(const sgc_plan *pl, const sgc_cache *c)
 // with_tiles: the cache's device tables are current and ordered in front of what comes next on the stream, as a suffix prefill
 // has them; the tile records are then written behind the copy.
 // cache (may be null): its page tables, if due, go with the same launch.
+// Partial results of a key range of a pass over drafted tokens: outputs [n_queries][rows][Hq][d] fp32, then log-sum-exps [Hq][n_queries rows].
+struct DraftParts {
+    size_t o, set;
+};
+static DraftParts draft_part_bytes(const sgc_plan *pl)
+{
+    const size_t rows = (size_t)pl->n_queries * pl->draft_rows * pl->ctx->p.n_q_heads;
+    const size_t o = (rows * pl->ctx->p.head_dim * sizeof(float) + 255) / 256 * 256;
+    return {o, o + (rows * sizeof(float) + 255) / 256 * 256};
+}
+
 static int plan_upload(sgc_plan *pl, hipStream_t s, bool with_tiles, sgc_cache *cache)
 {
     sgc_ctx *ctx = pl->ctx;
@@ -1295,9 +1395,12 @@ static int plan_upload(sgc_plan *pl, hipStream_t s, bool with_tiles, sgc_cache *
     plan_free_device(pl);
     pl->dtiles.clear();
     pl->dtok.clear();
+    pl->ftiles.clear();
+    pl->ftok.clear();
     if (want_rows > 0) {
         if (pl->tile_rows != want_rows) build_tiles(pl, want_rows);      // (a small call may have built them)
         if (pl->decode_cap > 0) build_decode_tiles(pl, want_rows);
+        if (pl->draft_rows > 0) build_draft_tiles(pl, want_rows);
         fill_tile_pt_off(pl, pl->cache);
     }
     pl->gtiles.clear();
@@ -1341,6 +1444,8 @@ static int plan_upload(sgc_plan *pl, hipStream_t s, bool with_tiles, sgc_cache *
         {pl->sq_query.data(), pl->sq_query.size() * 4, (const void **)&pl->d_sq_query},
         {pl->dtiles.data(), pl->dtiles.size() * sizeof(Tile), (const void **)&pl->d_dtiles},
         {pl->dtok.data(), pl->dtok.size() * sizeof(TokInfo), (const void **)&pl->d_dtok},
+        {pl->ftiles.data(), pl->ftiles.size() * sizeof(Tile), (const void **)&pl->d_ftiles},
+        {pl->ftok.data(), pl->ftok.size() * sizeof(TokInfo), (const void **)&pl->d_ftok},
         // the tile records are written on the device, from the seeds
         {nullptr, pl->tiles.size() * sizeof(Tile), (const void **)&pl->d_tiles},
     };
@@ -1381,6 +1486,7 @@ static int plan_upload(sgc_plan *pl, hipStream_t s, bool with_tiles, sgc_cache *
         pl->d_spool = pl->spool_block.p;
         if (pl->decode_cap > 0) SGC_HIP(ctx, launch_fill_zero_bytes(pl->d_spool, pl->spool_bytes, s));
     }
+    if (pl->draft_rows > 0 && (rc = dev_acquire(ctx, draft_part_bytes(pl).set * pl->draft_splits, s, &pl->draft_scratch)) != SGC_OK) return rc;
     pl->uploaded = true;
     return SGC_OK;
 }
@@ -1423,12 +1529,12 @@ int sgc_plan_destroy(sgc_plan *pl)
 static int refresh_tiles(sgc_plan *pl, const sgc_cache *c, hipStream_t s)
 {
     sgc_ctx *ctx = pl->ctx;
-    if (pl->tiles.empty() || pl->tiles_generation == c->generation) return SGC_OK;
+    if ((pl->tiles.empty() && pl->ftiles.empty()) || pl->tiles_generation == c->generation) return SGC_OK;
     fill_tile_pt_off(pl, c);
-    pl->expand_pending = true;
-    for (int which = 1; which < 2; ++which) {
-        const std::vector<Tile> &list = pl->dtiles;
-        const Tile *dev = pl->d_dtiles;
+    pl->expand_pending = !pl->tiles.empty();
+    for (int which = 0; which < 2; ++which) {
+        const std::vector<Tile> &list = which ? pl->ftiles : pl->dtiles;
+        const Tile *dev = which ? pl->d_ftiles : pl->d_dtiles;
         if (list.empty()) continue;
         const size_t bytes = list.size() * sizeof(Tile);
         char *host = nullptr;
@@ -1884,6 +1990,118 @@ int sgc_decode_step_batched_noalloc(sgc_ctx *ctx, const sgc_cache *cc, sgc_plan 
                                     void *hip_stream)
 {
     return decode_step(ctx, cc, pl, layer, step, dev_q, dev_k, dev_v, dev_o, dev_lse, hip_stream, true);
+}
+
+// ---- passes over drafted tokens -------------------------------------------------------------------
+int sgc_plan_enable_drafts(sgc_plan *pl, int32_t max_new_tokens, int32_t max_rows)
+{
+    if (!pl) return fail(nullptr, SGC_EINVAL, "plan is NULL");
+    sgc_ctx *ctx = pl->ctx;
+    if (max_rows < 1 || max_rows > kDraftMaxRows) return fail(ctx, SGC_EINVAL, "max_rows %d outside [1, %d]", max_rows, kDraftMaxRows);
+    if (max_new_tokens < max_rows) return fail(ctx, SGC_EINVAL, "max_new_tokens %d < max_rows %d", max_new_tokens, max_rows);
+    if ((int64_t)pl->n_queries * max_rows * ctx->p.n_q_heads > INT32_MAX / 32)
+        return fail(ctx, SGC_EINVAL, "batch too large: %d queries of %d rows", pl->n_queries, max_rows);
+    const int rc = sgc_plan_enable_decode(pl, max_new_tokens);
+    if (rc != SGC_OK || pl->draft_rows == max_rows) return rc;
+    plan_free_device(pl);          // the row lists change: rebuilt at the next upload
+    pl->tile_rows = 0;
+    pl->draft_rows = max_rows;
+    return SGC_OK;
+}
+
+int sgc_draft_step_batched(sgc_ctx *ctx, const sgc_cache *cc, sgc_plan *pl, int32_t layer, const int32_t *dev_done, const int32_t *dev_rows,
+                           const void *dev_q, const void *dev_k, const void *dev_v, void *dev_o, float *dev_lse, void *hip_stream)
+{
+    if (!ctx) return fail(nullptr, SGC_EINVAL, "ctx is NULL");
+    if (!cc || cc->ctx != ctx) return fail(ctx, SGC_EINVAL, "cache is NULL or belongs to another context");
+    if (!pl || pl->ctx != ctx || pl->cache != cc) return fail(ctx, SGC_EINVAL, "plan is NULL or was made for another context/cache");
+    if (layer < 0 || layer >= ctx->p.n_layers) return fail(ctx, SGC_EINVAL, "layer %d outside [0, %d)", layer, ctx->p.n_layers);
+    if (pl->draft_rows <= 0) return fail(ctx, SGC_ESTATE, "drafts were not enabled on this plan");
+    if (!pl->uploaded) return fail(ctx, SGC_ESTATE, "no suffix prefill has run on this plan: its suffix pages are empty");
+    sgc_cache *c = const_cast<sgc_cache *>(cc);
+    for (int32_t k = 0; k < pl->n_clusters; ++k) {
+        if (pl->cluster_off[k + 1] == pl->cluster_off[k]) continue;
+        if (!c->cl[k].allocated || c->cl[k].prefix_len != pl->cl_prefix_len[k])
+            return fail(ctx, SGC_ESTATE, "cluster %d changed since the plan was made", k);
+    }
+    const int32_t n_sq = (int32_t)pl->sq_len.size();
+    if (n_sq == 0) return SGC_OK;
+    if (!dev_done || !dev_q || !dev_k || !dev_v || !dev_o) return fail(ctx, SGC_EINVAL, "dev_done / dev_q / dev_k / dev_v / dev_o is NULL");
+    if (!aligned16(dev_done) || !aligned16(dev_rows) || !aligned16(dev_q) || !aligned16(dev_k) || !aligned16(dev_v) || !aligned16(dev_o) || !aligned16(dev_lse))
+        return fail(ctx, SGC_EINVAL, "device pointers must be 16-byte aligned");
+    const size_t rows = (size_t)pl->n_queries * pl->draft_rows, o_bytes = rows * ctx->p.n_q_heads * ctx->p.head_dim * 2;
+    const size_t kv_bytes = o_bytes / ctx->p.n_q_heads * ctx->p.n_kv_heads, lse_bytes = rows * ctx->p.n_q_heads * sizeof(float);
+    for (const void *in : {dev_q, dev_k, dev_v}) {
+        const size_t n = in == dev_q ? o_bytes : kv_bytes;
+        if (overlap(dev_o, o_bytes, in, n) || overlap(dev_lse, lse_bytes, in, n))
+            return fail(ctx, SGC_EINVAL, "dev_o and dev_lse may not overlap dev_q, dev_k or dev_v");
+    }
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    const bool rope_short = ctx->p.rope_base > 0.0f && pl->max_position + pl->decode_cap > ctx->rope_len;
+    const bool stale = !c->d_tables || c->dirty || pl->tiles_generation != c->generation;
+    int rc;
+    if (rope_short || stale) {
+        // refreshing allocates and copies from the host: not what a graph may record
+        if (capture_of(s) != hipStreamCaptureStatusNone)
+            return fail(ctx, SGC_ESTATE, "%s: run the call once outside the capture", rope_short ? "the rotary table is too short (set max_position)"
+                                                                                                 : "clusters were allocated or released since the plan's last launch");
+        if ((rc = ensure_rope(ctx, pl->max_position + pl->decode_cap, s)) != SGC_OK) return rc;
+        if ((rc = cache_sync(c, s)) != SGC_OK) return rc;
+        if ((rc = refresh_tiles(pl, c, s)) != SGC_OK) return rc;
+    }
+    pl->last_stream = s;
+    const DraftParts part = draft_part_bytes(pl);
+    char *const scratch = pl->draft_scratch.p;
+    char *const spool = pl->d_spool + (size_t)layer * pl->spool_layer_bytes;
+
+    AttnArgs a;
+    fill_common_args(a, ctx, c, layer);
+    a.q = dev_q;
+    a.lse_stride = (int64_t)rows;
+    a.mode = MODE_SUFFIX;
+    a.tiles = pl->d_ftiles;
+    a.n_tiles = (int32_t)pl->ftiles.size();
+    a.tok_info = pl->d_ftok;
+    a.spool = spool;
+    a.skip_self = 1;
+    a.done = dev_done;
+    a.done_cap = pl->decode_cap;
+    a.o = scratch;
+    a.lse = reinterpret_cast<float *>(scratch + part.o);
+    a.split_o_bytes = (int64_t)part.set;
+    a.split_lse_elems = (int64_t)(part.set / sizeof(float));
+
+    DraftArgs d{};
+    d.q = dev_q;
+    d.k = dev_k;
+    d.v = dev_v;
+    d.o = dev_o;
+    d.lse = dev_lse;
+    d.done = dev_done;
+    d.rows = dev_rows;
+    d.o_cached = scratch;
+    d.lse_cached = a.lse;
+    d.split_o_elems = (int64_t)(part.set / sizeof(float));
+    d.split_lse_elems = a.split_lse_elems;
+    d.lse_stride = (int64_t)rows;
+    d.spool = spool;
+    d.sq_query = pl->d_sq_query;
+    d.sq_len = pl->d_sq_len;
+    d.sq_page0 = pl->d_sq_page0;
+    d.sq_cluster = pl->d_sq_cluster;
+    d.cl_prefix_len = c->d_prefix_len;
+    d.rope = a.rope;
+    d.n_splits = pl->draft_splits;
+    d.n_sq = n_sq;
+    d.max_rows = pl->draft_rows;
+    d.cap = pl->decode_cap;
+    d.n_q_heads = ctx->p.n_q_heads;
+    d.n_kv_heads = ctx->p.n_kv_heads;
+    d.scale_log2e = a.scale_log2e;
+
+    SGC_HIP(ctx, launch_attn_mfma(a, s));
+    SGC_HIP(ctx, launch_draft_own_keys(d, s));
+    return SGC_OK;
 }
 
 int sgc_timing_enable(sgc_ctx *ctx, int on)

@@ -168,7 +168,7 @@ struct TokInfo {
     int32_t src;    // row of the token in the caller's packed arrays
     int32_t qpos;   // index of the token inside its query
     int32_t own0;   // first own page of the query (records of decode steps: its first page in the suffix page pool)
-    int32_t unused;
+    int32_t draft;  // records of passes over drafted tokens: query << 5 | number of the token in the pass
 };
 
 // One cluster of a (batched) prefix prefill.
@@ -209,6 +209,25 @@ struct DecodeArgs {
     int32_t n_sq, n_queries, step, n_q_heads, n_kv_heads;
     int32_t key_cap;              // multiple of 16, >= every query's len + step + 1, <= kDecodeMaxKeys
     int32_t use_mfma;             // head_dim 128 and 16-bit rows: the matrix-core form of the own-keys kernel may run
+    float scale_log2e;
+};
+
+// A pass over drafted tokens: arguments of the kernel for the queries' own keys (sgc_draft.hip).
+constexpr int kDraftMaxRows = 16;         // new tokens of a query: one page of keys
+struct DraftArgs {
+    const void *q, *k, *v;        // [n_queries][max_rows][Hq][d], [n_queries][max_rows][Hkv][d], bf16, before rotation
+    void *o;                      // [n_queries][max_rows][Hq][d]
+    float *lse;                   // [Hq][lse_stride] natural log, or null
+    const int32_t *done;          // [n_queries] generated tokens whose keys are in the pages
+    const int32_t *rows;          // [n_queries] new tokens, or null: max_rows of every query
+    const void *o_cached;         // cached part of the same rows, n_splits key ranges (as in DecodeArgs, but fp32)
+    const float *lse_cached;
+    int64_t split_o_elems, split_lse_elems, lse_stride;
+    char *spool;                  // the layer's suffix pages
+    const int32_t *sq_query, *sq_len, *sq_page0, *sq_cluster;
+    const int32_t *cl_prefix_len;
+    const float2 *rope;
+    int32_t n_splits, n_sq, max_rows, cap, n_q_heads, n_kv_heads;      // cap: generated tokens the pages have room for
     float scale_log2e;
 };
 
@@ -343,6 +362,10 @@ struct AttnArgs {
     int32_t n_ranges;
     // fp8 cache: run the first product on the e4m3 codes, with the query quantised per row (suffix mode)
     int32_t fp8_first_product;
+    // passes over drafted tokens: a row's position lies done[query] + its number in the pass behind its query's question (never at or
+    // behind done_cap: rows that the pass does not have are computed somewhere and not used).  Null otherwise.
+    const int32_t *done;
+    int32_t done_cap;
 };
 
 // ---- small calls: tables with the launch ----------------------------------------------------------------------------------
@@ -507,6 +530,16 @@ struct sgc_plan {
     int32_t dec_own_cost2 = 0;
     bool dec_few = false;                     // decode steps are one launch of the kernel for few rows
     std::vector<sgc::TokInfo> dtok;
+    // passes over drafted tokens (off unless sgc_plan_enable_drafts was called): up to draft_rows new tokens of a query; the same lists for
+    // the rows of a pass, and the partial results of its key ranges, which are there from the upload on
+    int32_t draft_rows = 0;
+    std::vector<sgc::Tile> ftiles;
+    std::vector<int32_t> ftile_key0;
+    std::vector<sgc::TokInfo> ftok;
+    int32_t draft_splits = 1;
+    sgc_dev_block draft_scratch;
+    const sgc::Tile *d_ftiles = nullptr;
+    const sgc::TokInfo *d_ftok = nullptr;
     size_t spool_layer_bytes = 0;
     sgc_dev_block dec_scratch;                // cached-prefix part of a decode step: O then LSE
     uint64_t dec_counters_cleared = 0;        // its counters: see clear_step_counters
@@ -545,6 +578,9 @@ struct sgc_plan {
 
 // ---- kernel launchers (defined in the .hip files) --------------------------------------------
 namespace sgc {
+
+// Keeps the text of a failure with the context (ctx may be null) and returns the code.
+int report(sgc_ctx *ctx, int code, const char *fmt, ...) __attribute__((format(printf, 3, 4)));
 
 // Builds the (cos, sin) table for positions [0, n_pos) in double precision, stored as fp32.
 hipError_t launch_rope_table(float2 *table, int n_pos, int head_dim, double base, hipStream_t s);
@@ -608,6 +644,8 @@ hipError_t launch_attn_generic(const CarriedGeneric &c, int n_gtiles, hipStream_
 // Decode, per (query, head): attention over the query's own keys (the step's new token was appended to the suffix
 // pages by the cached-part launch before) merged with the cached-prefix part.  head_dim 128, bf16.
 hipError_t launch_decode_own_keys(const DecodeArgs &d, hipStream_t s);
+// Passes over drafted tokens, behind the cached part: own keys, new ones among them, the sum, and the new keys' way into the pages.
+hipError_t launch_draft_own_keys(const DraftArgs &d, hipStream_t s);
 hipError_t launch_fill_zero_bytes(void *p, size_t bytes, hipStream_t s);
 // bytes (a multiple of 4, both pointers 16-byte aligned) from mapped host memory to device memory, read by a kernel;
 // optionally a second piece in the same launch; expand (may be null): tile records to write behind the copy

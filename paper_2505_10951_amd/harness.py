@@ -190,6 +190,37 @@ class Session:
                                     do.data_ptr(), dlse.data_ptr() if dlse is not None else None, self.stream)
         return do
 
+    # ---- several drafted tokens of every query in one pass ---------------------------------------------------
+    def enable_drafts(self, max_new_tokens: int, max_rows: int) -> None:
+        sgc.sgc_plan_enable_drafts(self.ctx, self.plan, max_new_tokens, max_rows)
+
+    def draft_step(self, done: torch.Tensor, rows: Optional[torch.Tensor], dq: torch.Tensor, dk: torch.Tensor, dv: torch.Tensor, layer: int = 0,
+                   do: Optional[torch.Tensor] = None, dlse: Optional[torch.Tensor] = None):
+        if do is None:
+            do = torch.zeros_like(dq)
+        sgc.sgc_draft_step_batched(self.ctx, self.cache, self.plan, layer, done.data_ptr(), rows.data_ptr() if rows is not None else None,
+                                   dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), do.data_ptr(), dlse.data_ptr() if dlse is not None else None,
+                                   self.stream)
+        return do
+
+    def draft_pass(self, p: "DraftPass", layer: int = 0) -> None:
+        """One pass over drafted tokens through one layer and the head: p.x -> queries, keys and values -> attention -> output projection ->
+        logits -> probabilities -> which drafts stand.  Everything it leaves is in p (out_tokens, accepted, done); nothing waits
+        for the host, so the call can be captured and replayed."""
+        n, R = p.done.numel(), p.tokens.shape[1]
+        p.project(p.x, p.w_q, p.q)
+        p.project(p.x, p.w_k, p.k)
+        p.project(p.x, p.w_v, p.v)
+        self.draft_step(p.done, p.rows, p.q, p.k, p.v, layer, do=p.o)
+        p.project(p.o, p.w_o, p.h)
+        p.project(p.h, p.w_head, p.logits)
+        vocab = p.logits.shape[1]
+        sgc.sgc_token_probs(self.ctx, n * R, vocab, p.logits.data_ptr(), sgc.SGC_F32, vocab, p.temperature, p.probs.data_ptr(), vocab,
+                            p.workspace.data_ptr(), p.workspace.numel(), self.stream)
+        sgc.sgc_verify_drafts(self.ctx, n, R, vocab, p.probs.data_ptr(), vocab, None, 0, p.tokens.data_ptr(), p.rows.data_ptr(),
+                              p.uniform.data_ptr(), p.out_tokens.data_ptr(), p.accepted.data_ptr(), p.done.data_ptr(), p.workspace.data_ptr(),
+                              p.workspace.numel(), self.stream)
+
     def export_cluster(self, c: int, layer: int = 0):
         """Canonical [P][Hkv][d] view of the cluster's cache: (k, v, k_scale, v_scale) on the host.
         k, v are fp32 values for f32/bf16 caches and raw uint8 e4m3 codes for fp8 caches.  (A 16-bit cache
@@ -238,6 +269,49 @@ class Session:
     def __exit__(self, *exc):
         self.close()
         return False
+
+
+class Fp8Weight:
+    """A projection's weight [n_features][d_model] as e4m3 codes with a power-of-two scale per 128 x 128 block."""
+
+    def __init__(self, w: torch.Tensor):
+        self.n_features, self.d_model = w.shape
+        kb = -(-self.d_model // 128)
+        self.codes = torch.empty((self.n_features, kb * 128), dtype=torch.uint8, device=w.device)
+        self.exponents = torch.empty((-(-self.n_features // 128), kb), dtype=torch.uint8, device=w.device)
+        sgc.sgc_quantise_weight_fp8(None, w.data_ptr(), {torch.float32: sgc.SGC_F32, torch.bfloat16: sgc.SGC_BF16}[w.dtype], self.n_features,
+                                    self.d_model, self.codes.data_ptr(), self.exponents.data_ptr(), torch.cuda.current_stream().cuda_stream)
+
+
+class DraftPass:
+    """Weights and buffers of Session.draft_pass: one layer's projections and a head over `vocab` tokens, all in 8 bits.  x: hidden states
+    of the pass's tokens [n_queries * max_rows][d_model]; tokens, rows, uniform: what sgc_verify_drafts takes."""
+
+    def __init__(self, w: Workload, d_model: int, vocab: int, max_rows: int, weights, temperature: float = 1.0, device: str = "cuda:0"):
+        n, bf16 = w.n_queries, torch.bfloat16
+        self.temperature = temperature
+        self.w_q, self.w_k, self.w_v, self.w_o, self.w_head = (Fp8Weight(x) for x in weights)
+
+        def rows(width, dtype=bf16):
+            return torch.zeros((n * max_rows, width), dtype=dtype, device=device)
+
+        self.x, self.h = rows(d_model), rows(d_model)
+        self.q, self.o = rows(w.n_q_heads * w.head_dim), rows(w.n_q_heads * w.head_dim)
+        self.k, self.v = rows(w.n_kv_heads * w.head_dim), rows(w.n_kv_heads * w.head_dim)
+        self.logits, self.probs = rows(vocab, torch.float32), rows(vocab, torch.float32)
+        self.tokens, self.out_tokens = (torch.zeros((n, max_rows), dtype=torch.int32, device=device) for _ in range(2))
+        self.uniform = torch.zeros((n, max_rows), device=device)
+        self.rows = torch.full((n,), max_rows, dtype=torch.int32, device=device)
+        self.done, self.accepted = (torch.zeros(n, dtype=torch.int32, device=device) for _ in range(2))
+        need = max(sgc.sgc_project_fp8_workspace(n * max_rows, x.n_features, x.d_model) for x in (self.w_q, self.w_k, self.w_v, self.w_o, self.w_head))
+        need = max(need, sgc.sgc_token_probs_workspace(n * max_rows, vocab), sgc.sgc_verify_workspace(n, vocab), 1)
+        self.workspace = torch.empty(need, dtype=torch.uint8, device=device)
+
+    def project(self, x: torch.Tensor, w: Fp8Weight, y: torch.Tensor) -> None:
+        types = {torch.float32: sgc.SGC_F32, torch.bfloat16: sgc.SGC_BF16}
+        sgc.sgc_project_fp8(None, x.data_ptr(), types[x.dtype], x.shape[1], x.shape[0], w.codes.data_ptr(), w.exponents.data_ptr(), w.n_features,
+                            w.d_model, y.data_ptr(), types[y.dtype], y.shape[1], self.workspace.data_ptr(), self.workspace.numel(),
+                            torch.cuda.current_stream().cuda_stream)
 
 
 def run_workload(w: Workload, layer: int = 0, kernel: int = sgc.SGC_KERNEL_AUTO, want_lse: bool = True) -> Dict:

@@ -28,6 +28,8 @@ EXPORTS = [
     "sgc_timing_enable", "sgc_timing_last", "sgc_cluster_queries", "sgc_plan_enable_decode", "sgc_decode_step_batched",
     "sgc_union_subgraphs", "sgc_project_qkv_prefix", "sgc_project_qkv_prefix_batched", "sgc_project_qkv_suffix",
     "sgc_project_out", "sgc_timing_get", "sgc_decode_step_batched_noalloc",
+    "sgc_plan_enable_drafts", "sgc_draft_step_batched", "sgc_token_probs_workspace", "sgc_token_probs", "sgc_verify_workspace",
+    "sgc_verify_drafts", "sgc_quantise_weight_fp8", "sgc_project_fp8_workspace", "sgc_project_fp8",
 ]
 
 
@@ -108,6 +110,18 @@ def lib() -> ctypes.CDLL:
         L.sgc_timing_enable.argtypes = [vp, ctypes.c_int]
         L.sgc_timing_last.argtypes = [vp, f32p, f32p]
         L.sgc_timing_get.argtypes = [vp, i32, f32p, f32p]
+        sz, f32 = ctypes.c_size_t, ctypes.c_float
+        L.sgc_plan_enable_drafts.argtypes = [vp, i32, i32]
+        L.sgc_draft_step_batched.argtypes = [vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.sgc_token_probs_workspace.argtypes = [i64, i32]
+        L.sgc_token_probs.argtypes = [vp, i64, i32, vp, i32, i64, f32, vp, i64, vp, sz, vp]
+        L.sgc_verify_workspace.argtypes = [i32, i32]
+        L.sgc_verify_drafts.argtypes = [vp, i32, i32, i32, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.sgc_quantise_weight_fp8.argtypes = [vp, vp, i32, i32, i32, vp, vp, vp]
+        L.sgc_project_fp8_workspace.argtypes = [i64, i32, i32]
+        L.sgc_project_fp8.argtypes = [vp, vp, i32, i64, i64, vp, vp, i32, i32, vp, i32, i64, vp, sz, vp]
+        for name in ("sgc_token_probs_workspace", "sgc_verify_workspace", "sgc_project_fp8_workspace"):
+            getattr(L, name).restype = sz
         for name in EXPORTS:
             fn = getattr(L, name)
             if fn.restype is ctypes.c_int and name not in ("sgc_version",):
@@ -309,6 +323,55 @@ def sgc_decode_step_batched_noalloc(ctx, cache, plan, layer: int, step: int, dev
                                     dev_lse: Optional[int] = None, stream: int = 0) -> None:
     _check(ctx, lib().sgc_decode_step_batched_noalloc(ctx, cache, plan, layer, step, dev_q, dev_k, dev_v, dev_o, dev_lse,
                                                       stream))
+
+
+def sgc_plan_enable_drafts(ctx, plan, max_new_tokens: int, max_rows: int) -> None:
+    _check(ctx, lib().sgc_plan_enable_drafts(plan, int(max_new_tokens), int(max_rows)))
+
+
+def sgc_draft_step_batched(ctx, cache, plan, layer: int, dev_done: int, dev_rows: Optional[int], dev_q: int, dev_k: int, dev_v: int,
+                           dev_o: int, dev_lse: Optional[int] = None, stream: int = 0) -> None:
+    """Up to max_rows new tokens of every query at once (dev_rows[n] of query n, None: max_rows), behind dev_done[n] generated ones."""
+    _check(ctx, lib().sgc_draft_step_batched(ctx, cache, plan, layer, dev_done, dev_rows, dev_q, dev_k, dev_v, dev_o, dev_lse, stream))
+
+
+def sgc_token_probs_workspace(n_rows: int, vocab: int) -> int:
+    return int(lib().sgc_token_probs_workspace(n_rows, vocab))
+
+
+def sgc_token_probs(ctx, n_rows: int, vocab: int, dev_logits: int, logits_dtype: int, logits_stride: int, temperature: float, dev_probs: int,
+                    probs_stride: int, dev_workspace: Optional[int] = None, workspace_bytes: int = 0, stream: int = 0) -> None:
+    """Probabilities (fp32) of rows of logits; temperature 0: one at the largest logit.  ctx may be None."""
+    _check(ctx, lib().sgc_token_probs(ctx, n_rows, vocab, dev_logits, logits_dtype, logits_stride, temperature, dev_probs, probs_stride,
+                                      dev_workspace, workspace_bytes, stream))
+
+
+def sgc_verify_workspace(n_queries: int, vocab: int) -> int:
+    return int(lib().sgc_verify_workspace(n_queries, vocab))
+
+
+def sgc_verify_drafts(ctx, n_queries: int, max_rows: int, vocab: int, dev_target: int, target_stride: int, dev_draft: Optional[int], draft_stride: int,
+                      dev_tokens: int, dev_rows: Optional[int], dev_uniform: int, dev_out_tokens: int, dev_accepted: int,
+                      dev_done: Optional[int] = None, dev_workspace: Optional[int] = None, workspace_bytes: int = 0, stream: int = 0) -> None:
+    """Which drafted tokens stand, and the token behind them.  ctx may be None."""
+    _check(ctx, lib().sgc_verify_drafts(ctx, n_queries, max_rows, vocab, dev_target, target_stride, dev_draft, draft_stride, dev_tokens, dev_rows,
+                                        dev_uniform, dev_out_tokens, dev_accepted, dev_done, dev_workspace, workspace_bytes, stream))
+
+
+def sgc_quantise_weight_fp8(ctx, dev_w: int, w_dtype: int, n_features: int, d_model: int, dev_codes: int, dev_exponents: int, stream: int = 0) -> None:
+    """Weights [n_features][d_model] -> e4m3 codes [n_features][ceil(d_model / 128) * 128] and exponents + 127, a byte per 128 x 128."""
+    _check(ctx, lib().sgc_quantise_weight_fp8(ctx, dev_w, w_dtype, n_features, d_model, dev_codes, dev_exponents, stream))
+
+
+def sgc_project_fp8_workspace(n_rows: int, n_features: int, d_model: int) -> int:
+    return int(lib().sgc_project_fp8_workspace(n_rows, n_features, d_model))
+
+
+def sgc_project_fp8(ctx, dev_x: int, x_dtype: int, x_stride: int, n_rows: int, dev_codes: int, dev_exponents: int, n_features: int, d_model: int,
+                    dev_y: int, y_dtype: int, y_stride: int, dev_workspace: Optional[int] = None, workspace_bytes: int = 0, stream: int = 0) -> None:
+    """y [n_rows][n_features] = x W^T with W as sgc_quantise_weight_fp8 leaves it; x is quantised on the way.  ctx may be None."""
+    _check(ctx, lib().sgc_project_fp8(ctx, dev_x, x_dtype, x_stride, n_rows, dev_codes, dev_exponents, n_features, d_model, dev_y, y_dtype,
+                                      y_stride, dev_workspace, workspace_bytes, stream))
 
 
 LINKAGES = {"ward": 0, "single": 1, "average": 2, "complete": 3, "centroid": 4}

@@ -1,0 +1,432 @@
+"""What stands around a pass over drafted tokens: products with 8-bit weights, probabilities of logits, verification; and a run of all of
+it together.  References in numpy, 64 bits."""
+import math
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from oracle import oracle as orc
+from paper_2505_10951_amd import sgc, workloads
+from paper_2505_10951_amd.harness import DraftPass, Fp8Weight, Session, to_device
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"f32": (torch.float32, sgc.SGC_F32), "bf16": (torch.bfloat16, sgc.SGC_BF16)}
+
+
+def _stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+# ---- products -----------------------------------------------------------------------------------------------------------
+def _exponents(amax):
+    """Smallest e with amax <= 448 * 2^e, by exact arithmetic on the mantissa."""
+    m, e = np.frexp(amax / 448.0)
+    return np.where(amax > 0, np.clip(np.where(m == 0.5, e - 1, e), -127, 127), 0).astype(int)
+
+
+def _e4m3(y):
+    """|y| <= 448 rounded to e4m3, nearest, ties to even (64 bits): four significant bits, multiples of 2^-9 below 2^-6."""
+    _, e = np.frexp(np.abs(y))
+    step = np.exp2(np.maximum(e, -5) - 4.0)
+    return np.round(y / step) * step
+
+
+def _pad(x, rows=1):
+    x = np.asarray(x, dtype=np.float64)
+    return np.pad(x, ((0, -x.shape[0] % rows), (0, -x.shape[1] % 128)))
+
+
+def _quantised_rows(x):
+    b = _pad(x).reshape(x.shape[0], -1, 128)
+    e = _exponents(np.abs(b).max(axis=2, keepdims=True))
+    return (_e4m3(b * np.exp2(-e)) * np.exp2(e)).reshape(x.shape[0], -1)
+
+
+def _quantised_weight(w):
+    p = _pad(w, 128)
+    b = p.reshape(p.shape[0] // 128, 128, -1, 128)
+    e = _exponents(np.abs(b).max(axis=(1, 3)))
+    s = np.exp2(e)[:, None, :, None]
+    codes = _e4m3(b / s)
+    return codes.reshape(p.shape)[: w.shape[0]], e, (codes * s).reshape(p.shape)[: w.shape[0]]
+
+
+def _decode(codes):
+    return torch.from_numpy(codes).view(torch.float8_e4m3fn).double().numpy()
+
+
+@pytest.mark.parametrize("n,k", [(1, 16), (128, 128), (200, 272), (129, 1024), (40, 144)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_weights_are_quantised_exactly(n, k, dtype):
+    g = np.random.default_rng(n * k)
+    w = torch.from_numpy((g.standard_normal((n, k)) * np.exp2(g.integers(-20, 20, size=(n, 1)))).astype(np.float32)).to(TYPES[dtype][0])
+    w[0, 0] = 448.0 * 2.0 ** 30             # a block whose largest is exactly representable, and one of zeros
+    if k > 128:
+        w[:, 128:256] = 0.0
+    q = Fp8Weight(w.to(DEV))
+    torch.cuda.synchronize()
+    codes, e, _ = _quantised_weight(w.double().numpy())
+    assert np.array_equal(q.exponents.cpu().numpy().astype(int) - 127, e)
+    assert np.array_equal(_decode(q.codes.cpu().numpy()), codes)
+
+
+def _project(x, w, y_dtype, x_pad=0, y_pad=0, w8=None):
+    m, k = x.shape
+    q = w8 or Fp8Weight(w)
+    n = q.n_features
+    xs = torch.full((m, k + x_pad), float("nan"), dtype=x.dtype, device=DEV)
+    xs[:, :k] = x
+    y = torch.full((m + 1, n + y_pad), 7.0, dtype=TYPES[y_dtype][0], device=DEV)
+    need = sgc.sgc_project_fp8_workspace(m, n, k)
+    ws = torch.full((need + 64,), 0xFF, dtype=torch.uint8, device=DEV)
+    sgc.sgc_project_fp8(None, xs.data_ptr(), TYPES["f32" if x.dtype == torch.float32 else "bf16"][1], k + x_pad, m, q.codes.data_ptr(), q.exponents.data_ptr(), n, k,
+                        y.data_ptr(), TYPES[y_dtype][1], n + y_pad, ws.data_ptr(), need, _stream())
+    torch.cuda.synchronize()
+    assert (ws[need:] == 0xFF).all()
+    assert (y[m] == 7.0).all() and (y[:m, n:] == 7.0).all()          # nothing behind the rows
+    return y[:m, :n].double().cpu().numpy()
+
+
+SHAPES = [(1, 1, 16), (1, 128, 128), (3, 40, 272), (20, 384, 1024), (31, 130, 144), (33, 129, 2048), (64, 1000, 512), (65, 257, 512), (127, 128, 4096), (200, 333, 640),
+          (300, 520, 1040), (513, 640, 384), (1030, 260, 256), (16, 5001, 256), (700, 2100, 512), (2100, 1100, 384)]
+
+
+@pytest.mark.parametrize("m,n,k", SHAPES)
+@pytest.mark.parametrize("x_dtype,y_dtype", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")])
+def test_products(m, n, k, x_dtype, y_dtype):
+    g = torch.Generator().manual_seed(m + n + k)
+    x = torch.randn((m, k), generator=g) * torch.exp2(torch.randint(-8, 8, (m, 1), generator=g).float())
+    w = torch.randn((n, k), generator=g) * torch.exp2(torch.randint(-3, 3, (1, k), generator=g).float())
+    x, w = x.to(TYPES[x_dtype][0]), w.to(torch.bfloat16)
+    got = _project(x.to(DEV), w.to(DEV), y_dtype, x_pad=16 * (m % 3), y_pad=n % 5)
+    xq, wq = _quantised_rows(x.double().numpy()), _quantised_weight(w.double().numpy())[2]
+    ref, mag = xq @ wq.T, np.abs(xq) @ np.abs(wq).T
+    # fp32 result: products exact, at most k + 16 additions of relative error 2^-24 each (a partial sum is at most the sum of magnitudes);
+    # bf16 result: the 8-bit instruction drops what lies 2^-16 below the largest product it adds, once per product (so at most k 2^-16 of the largest of
+    # 64, bounded here by 2^-12 of the sum of magnitudes + its 64 neighbours), and half a step of the result
+    tol = mag * ((k + 16) * 2.0 ** -24) if y_dtype == "f32" else mag * 2.0 ** -10 + np.abs(ref) * 2.0 ** -8
+    assert (np.abs(got - ref) <= tol + 1e-30).all(), float((np.abs(got - ref) / (tol + 1e-30)).max())
+
+
+def test_products_repeat_and_do_not_depend_on_neighbouring_rows():
+    g = torch.Generator().manual_seed(1)
+    x, w = torch.randn((70, 512), generator=g).bfloat16().to(DEV), torch.randn((300, 512), generator=g).bfloat16().to(DEV)
+    w8 = Fp8Weight(w)
+    a, b = (_project(x, w, "f32", w8=w8) for _ in range(2))
+    assert np.array_equal(a, b)
+    y = x.clone()
+    y[5] = float("nan")
+    y[6, 3] = float("inf")
+    c = _project(y, w, "f32", w8=w8)
+    assert np.isnan(c[5:7]).all()
+    keep = [i for i in range(70) if i not in (5, 6)]
+    assert np.array_equal(a[keep], c[keep])
+    w[7, 9] = float("inf")
+    d = _project(x, w, "bf16")
+    assert np.isnan(d[:, 7]).all() and np.isfinite(np.delete(d, 7, axis=1)).all()
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -120, 2.0 ** -60, 2.0 ** 60, 2.0 ** 100])
+def test_products_of_far_magnitudes(scale):
+    g = torch.Generator().manual_seed(2)
+    x, w = (torch.randn((40, 256), generator=g).double() * scale).float(), (torch.randn((136, 256), generator=g).double() / scale).float()
+    if not torch.isfinite(w).all():
+        w = torch.randn((136, 256), generator=g)
+    got = _project(x.to(DEV), w.to(DEV), "f32")
+    xq, wq = _quantised_rows(x.double().numpy()), _quantised_weight(w.double().numpy())[2]
+    assert (np.abs(got - xq @ wq.T) <= (np.abs(xq) @ np.abs(wq).T) * (272 * 2.0 ** -24)).all()
+
+
+# ---- probabilities ------------------------------------------------------------------------------------------------------
+def _probs_ref(x, T):
+    x = np.where(np.isnan(x), -np.inf, x.astype(np.float64))
+    p = np.zeros_like(x)
+    for i, r in enumerate(x):
+        top = r.max()
+        if top == -np.inf:
+            continue
+        if T == 0:
+            p[i, int(np.argmax(r))] = 1.0
+        else:
+            e = np.where(r == top, 1.0, np.exp(np.where(r == top, 0.0, r - top) / T))
+            p[i] = e / e.sum()
+    return p
+
+
+def _token_probs(x, T, pad=0, shift=0):
+    rows, vocab = x.shape
+    xs = torch.full((rows * (vocab + pad) + shift,), float("nan"), dtype=x.dtype, device=DEV)
+    view = xs[shift:].view(rows, vocab + pad)
+    view[:, :vocab] = x
+    p = torch.full((rows * (vocab + pad) + shift + 8,), 7.0, device=DEV)
+    need = sgc.sgc_token_probs_workspace(rows, vocab)
+    ws = torch.full((need + 64,), 0xFF, dtype=torch.uint8, device=DEV)
+    sgc.sgc_token_probs(None, rows, vocab, view.data_ptr(), TYPES["f32" if x.dtype == torch.float32 else "bf16"][1], vocab + pad, T,
+                        p[shift:].data_ptr(), vocab + pad, ws.data_ptr(), need, _stream())
+    torch.cuda.synchronize()
+    assert (ws[need:] == 0xFF).all() and (p[:shift] == 7.0).all() and (p[shift + rows * (vocab + pad):] == 7.0).all()
+    out = p[shift: shift + rows * (vocab + pad)].view(rows, vocab + pad)
+    assert (out[:, vocab:] == 7.0).all()
+    return out[:, :vocab].double().cpu().numpy()
+
+
+def _probs_tolerance(x, T, ref):
+    """exp2 of an argument that three roundings made (relative 3 * 2^-24 of up to A), its own two steps, a thread's sum of up to vocab / 512 + 64
+    values and the joins, one division: relative; values below 2^-126 may be flushed."""
+    v = x[np.isfinite(x)]
+    A = (v.max() - v.min()) / (T if T > 0 else 1.0) * 1.45 if v.size else 0.0
+    return ref * (2.0 ** -24 * (3 * A + x.shape[1] / 512 + 160)) + 2.0 ** -125
+
+
+@pytest.mark.parametrize("rows,vocab", [(1, 1), (2, 7), (3, 64), (5, 1001), (4, 50021), (1, 131072), (600, 333), (1100, 4097), (2, 8192)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [0.0, 0.7, 1.0])
+def test_probabilities(rows, vocab, dtype, T):
+    g = torch.Generator().manual_seed(rows + vocab)
+    x = (torch.randn((rows, vocab), generator=g) * 4).masked_fill(torch.rand((rows, vocab), generator=g) < 0.05, float("-inf")).to(TYPES[dtype][0])
+    got = _token_probs(x.to(DEV), T, pad=vocab % 3, shift=rows % 4)
+    xs = x.double().numpy()
+    ref = _probs_ref(xs, T)
+    assert (np.abs(got - ref) <= _probs_tolerance(xs, T, ref)).all()
+
+
+@pytest.mark.parametrize("rows,vocab", [(9, 300), (9, 20000)])            # one workgroup a row, and several
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_probabilities_of_odd_rows(rows, vocab, dtype):
+    x = torch.randn((rows, vocab), generator=torch.Generator().manual_seed(3)).to(TYPES[dtype][0])
+    lowest = torch.finfo(x.dtype).min
+    x[0] = float("-inf")
+    x[1] = float("nan")
+    x[2, 5], x[2, 9] = float("inf"), float("inf")
+    x[3] = lowest                                        # masked by the type's lowest value: all alike
+    x[4, 1:] = lowest
+    x[5] = float("-inf")
+    x[5, vocab - 1] = -3.0
+    x[6, :7] = float("nan")
+    x[7] = 1.0                                           # ties: the first one
+    x[8, 17] = x[8, vocab - 2] = 40.0
+    for T in (0.0, 0.5, 3.0):
+        got, ref = _token_probs(x.to(DEV), T), _probs_ref(x.double().numpy(), T)
+        assert (np.abs(got - ref) <= ref * 1e-4 + 2.0 ** -125).all()
+        assert (got[:2] == 0).all()
+
+
+def test_probabilities_at_extreme_temperatures():
+    x = torch.tensor([[1.0, 2.0, 2.0, -5.0]] * 3)
+    assert np.array_equal(_token_probs(x.to(DEV), 1e-40), np.array([[0, 0.5, 0.5, 0]] * 3))
+    assert np.abs(_token_probs(x.to(DEV), 1e30) - 0.25).max() < 1e-6
+
+
+# ---- verification -------------------------------------------------------------------------------------------------------
+def _verify_ref(p, q, tokens, rows, u, done):
+    n, R = tokens.shape
+    out, acc, done = np.full((n, R), -1), np.zeros(n, int), done.copy()
+    p, u = p.astype(np.float64), u.astype(np.float64)
+    V = p.shape[2]
+    for i in range(n):
+        r = min(int(rows[i]), R)
+        if r < 1:
+            continue
+        a = 0
+        while a < r - 1:
+            x = int(tokens[i, a + 1])
+            if not (0 <= x < V and u[i, a] * (1.0 if q is None else float(q[i, a, x])) < p[i, a, x]):
+                break
+            a += 1
+        w = np.where(p[i, a] > 0, p[i, a], 0.0)
+        if a < r - 1:
+            y = np.zeros(V)
+            if q is not None:
+                y = q[i, a].astype(np.float64)
+            elif 0 <= tokens[i, a + 1] < V:
+                y[tokens[i, a + 1]] = 1.0
+            res = np.where(p[i, a] > y, p[i, a] - y, 0.0)
+            if res.sum() > 0:
+                w = res
+        c = np.cumsum(w)
+        hit = np.flatnonzero(c > u[i, R - 1] * c[-1])
+        out[i, :a] = tokens[i, 1: a + 1]
+        out[i, a] = hit[0] if hit.size else (np.flatnonzero(w > 0)[-1] if (w > 0).any() else -1)
+        acc[i] = a
+        done[i] += a + 1
+    return out, acc, done
+
+
+def _verify(p, q, tokens, rows, u, done, pad=0):
+    n, R, V = p.shape
+    wide = lambda t: None if t is None else torch.nn.functional.pad(torch.from_numpy(np.ascontiguousarray(t)), (0, pad), value=99.0).to(DEV).contiguous()
+    dp, dq = wide(p), wide(q) if R > 1 else None
+    i32 = lambda a: torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).to(DEV)
+    dt, du, dd = i32(tokens), torch.from_numpy(u).to(DEV), i32(done)
+    dr = None if rows is None else i32(rows)
+    out, acc = torch.full((n + 1, R), 77, dtype=torch.int32, device=DEV), torch.full((n + 1,), 77, dtype=torch.int32, device=DEV)
+    need = sgc.sgc_verify_workspace(n, V)
+    ws = torch.full((need + 64,), 0xFF, dtype=torch.uint8, device=DEV)
+    sgc.sgc_verify_drafts(None, n, R, V, dp.data_ptr(), V + pad, None if dq is None else dq.data_ptr(), V + pad, dt.data_ptr(), None if dr is None else dr.data_ptr(),
+                          du.data_ptr(), out.data_ptr(), acc.data_ptr(), dd.data_ptr(), ws.data_ptr(), need, _stream())
+    torch.cuda.synchronize()
+    assert (ws[need:] == 0xFF).all() and (out[n] == 77).all() and acc[n] == 77
+    return out[:n].cpu().numpy(), acc[:n].cpu().numpy(), dd.cpu().numpy()
+
+
+def _same(a, b):
+    assert all(np.array_equal(x, y) for x, y in zip(a, b)), [np.flatnonzero((x != y).reshape(len(x), -1).any(axis=1)) for x, y in zip(a, b)]
+
+
+@pytest.mark.parametrize("n,R,V", [(1, 1, 1), (7, 4, 5), (300, 5, 64), (40, 16, 1001), (5, 6, 131072), (64, 3, 50021), (1, 2, 17)])
+@pytest.mark.parametrize("with_q", [False, True])
+def test_verification(n, R, V, with_q):
+    rng = np.random.default_rng(n * V + R)
+    soft = lambda x: (np.exp(x - x.max(-1, keepdims=True)) / np.exp(x - x.max(-1, keepdims=True)).sum(-1, keepdims=True)).astype(np.float32)
+    x = rng.standard_normal((n, R, V)) * 3
+    x[rng.random((n, R, V)) < 0.1] = -1e30
+    p, q = soft(x), soft(x[:, : R - 1] + rng.standard_normal((n, R - 1, V)) * 0.7)
+    tokens = rng.integers(0, V, size=(n, R))
+    for i in range(n):
+        for j in range(R - 1):
+            tokens[i, j + 1] = rng.choice(V, p=q[i, j].astype(np.float64) / q[i, j].astype(np.float64).sum())
+    u = rng.random((n, R)).astype(np.float32)
+    u[rng.random((n, R)) < 0.1] = 0.0
+    rows, done = rng.integers(-1, R + 2, size=n), rng.integers(0, 9, size=n)
+    for r in (rows, None):
+        _same(_verify(p, q if with_q else None, tokens, r, u, done, pad=V % 3),
+              _verify_ref(p, q if with_q else None, tokens, np.full(n, R) if r is None else r, u, done))
+
+
+def test_verification_at_the_edges():
+    # one query a line: vocabulary of 300, two drafts
+    V, R = 300, 3
+    n = 12
+    p, q = np.zeros((n, R, V), np.float32), np.zeros((n, R - 1, V), np.float32)
+    p[:, :, 100] = p[:, :, 200] = 0.5
+    q[:, :, 100] = q[:, :, 200] = 0.5
+    tokens, u = np.tile(np.array([1, 100, 200]), (n, 1)), np.full((n, R), 0.25, np.float32)
+    tokens[1, 1] = -1                    # no token: refused
+    tokens[2, 2] = V                     # neither is this
+    u[3] = 0.0
+    u[4] = np.float32(1 - 2.0 ** -24)    # the largest below one: equal probabilities stand all the same
+    p[5] = 0.0                           # a row without weights
+    p[6, 0] = 0.0
+    p[6, 0, 299] = 1e-30                 # refused; all the weight on the last token
+    p[7, :, 100] = np.nan                # a NaN weighs nothing and refuses
+    p[8, 0, 100] = 0.25                  # less than the draft said: stands below a half
+    u[8, 0] = 0.5
+    p[9, 0, 100] = 0.25
+    u[9, 0] = np.float32(0.5 - 2.0 ** -25)
+    q[10, 0, 100] = 0.0                  # a draft that its own probabilities rule out
+    u[11, 2] = 0.5                       # the border between two tokens belongs to the second
+    rows, done = np.full(n, R), np.arange(n)
+    for qq in (q, None):
+        _same(_verify(p, qq, tokens, rows, u, done), _verify_ref(p, qq, tokens, rows, u, done))
+    # a draft whose probabilities cover the target's: the target's own row is drawn from
+    p2, q2 = p[:1].copy(), q[:1].copy()
+    p2[0, 0, 100], q2[0, 0, 100], q2[0, 0, 200] = 0.25, 0.5, 0.75
+    u2 = np.array([[0.9, 0.5, 0.5]], np.float32)
+    got = _verify(p2, q2, tokens[:1], rows[:1], u2, done[:1])
+    _same(got, _verify_ref(p2, q2, tokens[:1], rows[:1], u2, done[:1]))
+    assert got[1][0] == 0 and got[0][0, 0] == 200
+
+
+def test_verification_follows_the_target():
+    # drawn drafts, tested and replaced: the first token behind is distributed as the target says, whatever the draft said
+    rng = np.random.default_rng(4)
+    n, V = 40000, 6
+    p0, q0 = np.array([0.4, 0.05, 0.2, 0.05, 0.3, 0.0]), np.array([0.1, 0.4, 0.2, 0.1, 0.1, 0.1])
+    p, q = np.tile(p0.astype(np.float32), (n, 2, 1)), np.tile(q0.astype(np.float32), (n, 1, 1))
+    tokens = np.stack([np.zeros(n, int), rng.choice(V, size=n, p=q0)], axis=1)
+    out, acc, _ = _verify(p, q, tokens, None, rng.random((n, 2)).astype(np.float32), np.zeros(n, int))
+    freq = np.bincount(out[:, 0], minlength=V) / n
+    # standard deviation of a frequency at most sqrt(0.25 / n) = 2.5e-3: five of them
+    assert np.abs(freq - p0).max() < 1.25e-2
+    assert abs(acc.mean() - np.minimum(p0, q0).sum()) < 1.25e-2
+
+
+# ---- together -----------------------------------------------------------------------------------------------------------
+def test_passes_through_a_layer_and_the_head():
+    """Three passes: hidden states -> q, k, v -> attention -> output projection -> logits -> probabilities -> verification, eager and as one captured
+    graph replayed; against the same in 64 bits."""
+    w = workloads.custom("draft_loop", n_q_heads=8, n_kv_heads=2, head_dim=128, rope_base=500000.0, io_dtype="bf16", prefix_len=[150, 40],
+                         labels=[0, 1, 0, 1, 0], suffix_len=[9, 16, 1, 30, 12], seed=12)
+    n, R, dm, V, cap, n_pass = w.n_queries, 4, 256, 1000, 16, 3
+    g = torch.Generator().manual_seed(8)
+    mk = lambda rows, cols: (torch.randn((rows, cols), generator=g) / math.sqrt(cols)).bfloat16().to(DEV)
+    weights = [mk(8 * 128, dm), mk(2 * 128, dm), mk(2 * 128, dm), mk(dm, 8 * 128), mk(V, dm) * 3]
+    embed = torch.randn((V, dm), generator=g).bfloat16().to(DEV)
+    uniform = torch.rand((n_pass, n, R), generator=g).to(DEV)
+    caches = []
+    for c in range(w.n_clusters):
+        k, v = w.prefix_kv(c)
+        caches.append(orc.prefix_prefill(None, k, v, w.rope_base)[:2])
+    deq = [_quantised_weight(t.double().cpu().numpy())[2] for t in weights]
+
+    def run(captured):
+        with Session(w) as s:
+            for c in range(w.n_clusters):
+                s.alloc_cluster(c)
+            s.prefix_prefill_batched(list(range(w.n_clusters)), 0)
+            s.assign()
+            s.enable_drafts(cap, R)
+            s.suffix_prefill(*(to_device(t, "bf16") for t in w.suffix_qkv(0)))
+            p = DraftPass(w, dm, V, R, weights, temperature=0.8)
+            # the first pass outside, so that the graph finds every table in place; its counts are taken back
+            s.draft_pass(p)
+            p.done.zero_()
+            torch.cuda.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            if captured:
+                with torch.cuda.graph(graph):
+                    s.draft_pass(p)
+            last = torch.arange(n, device=DEV, dtype=torch.int32)
+            trace = []
+            for i in range(n_pass):
+                # drafts: what a greedy look at the last pass's probabilities would say, or a fixed guess
+                p.tokens[:, 0] = last
+                for j in range(1, R):
+                    p.tokens[:, j] = (p.tokens[:, j - 1] * 7 + 3) % V
+                p.x.copy_(embed[p.tokens.reshape(-1).long()])
+                p.uniform.copy_(uniform[i] * (1.0 if i != 1 else 1e-4))          # (in the second pass nearly everything stands)
+                before = p.done.clone()
+                if captured:
+                    graph.replay()
+                else:
+                    s.draft_pass(p)
+                torch.cuda.synchronize()
+                trace.append([t.cpu().numpy().copy() for t in (p.tokens, before, p.logits, p.probs, p.out_tokens, p.accepted, p.done)])
+                last = p.out_tokens.gather(1, p.accepted[:, None].long()).squeeze(1)
+            return trace
+
+    eager, replayed = run(False), run(True)
+    for a, b in zip(eager, replayed):
+        for x, y in zip(a, b):
+            assert np.array_equal(x, y)
+    # 64 bits, along the tokens that the run chose
+    em = embed.double().cpu().numpy()
+    bf = lambda x: torch.from_numpy(x).bfloat16().double().numpy()
+    kept = [[np.zeros((0, 2, 128)), np.zeros((0, 2, 128))] for _ in range(n)]
+    for i, (tokens, before, logits, probs, out, accepted, done) in enumerate(eager):
+        for m in range(n):
+            assert before[m] == kept[m][0].shape[0]
+            xq = _quantised_rows(em[tokens[m]])
+            q, k, v = (bf(xq @ deq[t].T).reshape(R, -1, 128) for t in range(3))
+            sq, sk, sv = (t.astype(np.float64) for t in w.suffix_qkv_query(m, 0))
+            keys, vals = (np.concatenate([a, b, c]) for a, b, c in ((sk, kept[m][0], k), (sv, kept[m][1], v)))
+            qs = np.concatenate([sq, np.zeros((before[m], 8, 128)), q])
+            o, _, _ = orc.suffix_prefill(*caches[int(w.labels[m])], qs, keys, vals, w.rope_base)
+            h = bf(_quantised_rows(bf(o[-R:].reshape(R, -1))) @ deq[3].T)
+            ref = _quantised_rows(h) @ deq[4].T
+            got = logits.reshape(n, R, V)[m]
+            # bf16 rounding of q, k, v, o, h (2^-9 each, amplified by the attention), and codes that take their neighbour (up to 2^-4
+            # of an element, on few of them): a few percent of the logits' spread
+            assert np.linalg.norm(got - ref) <= 0.05 * np.linalg.norm(ref), (i, m, np.linalg.norm(got - ref) / np.linalg.norm(ref))
+            a = int(accepted[m])
+            kept[m] = [np.concatenate([kept[m][0], k[: a + 1]]), np.concatenate([kept[m][1], v[: a + 1]])]
+            assert done[m] == before[m] + a + 1
+        # each step against its own inputs
+        ref_p = _probs_ref(logits.astype(np.float64), 0.8)
+        assert (np.abs(probs - ref_p) <= _probs_tolerance(logits.astype(np.float64), 0.8, ref_p)).all()
+        u = (uniform[i] * (1.0 if i != 1 else 1e-4)).cpu().numpy()
+        ref_v = _verify_ref(probs.reshape(n, R, V), None, tokens, np.full(n, R), u, before)
+        _same((out, accepted, done), ref_v)
