@@ -5,6 +5,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "sgc_internal.h"
 
@@ -27,12 +28,14 @@ struct RowOf<float> {
     static constexpr int N = 4;
     typedef Row4 vec;
     static __device__ __forceinline__ float value(float x) { return x; }
+    static __device__ __forceinline__ float ruled_out() { return -INFINITY; }
 };
 template <>
 struct RowOf<uint16_t> {
     static constexpr int N = 8;
     typedef Row8 vec;
     static __device__ __forceinline__ float value(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+    static __device__ __forceinline__ uint16_t ruled_out() { return 0xFF80; }
 };
 
 __device__ __forceinline__ float logit(float x) { return x == x ? x : -INFINITY; }       // a NaN rules a token out
@@ -149,15 +152,105 @@ __global__ void __launch_bounds__(PT) token_probs_kernel(const T *logits, int64_
     });
 }
 
+// Rows that fit a workgroup's registers: read once, NV vectors of a thread.  Bounded by memory: the row's bytes in, four bytes a token out.
+constexpr int RT = 1024;
+template <typename T, int NV>
+__global__ void __launch_bounds__(RT) token_probs_row_kernel(const T *logits, int64_t logits_stride, float *probs, int64_t probs_stride, int vocab, float c)
+{
+    constexpr int N = RowOf<T>::N;
+    typedef typename RowOf<T>::vec vec;
+    __shared__ Part part[RT / 64];
+    const int64_t r = blockIdx.x;
+    const T *row = logits + r * logits_stride;
+    float *out = probs + r * probs_stride;
+    // (a thread's first token: the workgroup's pieces begin at 128-byte lines of the output, up to 31 tokens in front of the row)
+    const int first = (int)threadIdx.x * N - (int)((reinterpret_cast<uintptr_t>(out) >> 2) & 31);
+    vec v[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int i = first + k * RT * N;
+        if (i >= 0 && i + N <= vocab) {
+            v[k] = *reinterpret_cast<const vec *>(row + i);
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[k].x[e] = i + e >= 0 && i + e < vocab ? row[i + e] : RowOf<T>::ruled_out();
+        }
+    }
+    auto x = [&](int k, int e) __attribute__((always_inline)) { return logit(RowOf<T>::value(v[k].x[e])); };
+    Part mine = {-INFINITY, 0.f, 0x7fffffff};
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int e = 0; e < N; ++e) mine.top = fmaxf(mine.top, x(k, e));
+    if (mine.top > -INFINITY) {
+        if (c == 0.f) {
+#pragma unroll
+            for (int k = NV - 1; k >= 0; --k)
+#pragma unroll
+                for (int e = N - 1; e >= 0; --e)
+                    if (x(k, e) == mine.top) mine.at = first + k * RT * N + e;
+        } else {
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int e = 0; e < N; ++e) mine.sum += weight(x(k, e), mine.top, c);
+        }
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        Part other;
+        other.top = __shfl_xor(mine.top, d);
+        other.sum = __shfl_xor(mine.sum, d);
+        other.at = __shfl_xor(mine.at, d);
+        mine = join(mine, other, c);
+    }
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = mine;
+    __syncthreads();
+    mine = part[0];
+#pragma unroll
+    for (int w = 1; w < RT / 64; ++w) mine = join(mine, part[w], c);
+    const bool some = mine.top > -INFINITY;
+    const float inv = some ? 1.f / mine.sum : 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int i = first + k * RT * N;
+        float p[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) p[e] = c == 0.f ? (some && i + e == mine.at ? 1.f : 0.f) : (some ? weight(x(k, e), mine.top, c) * inv : 0.f);
+        if (i >= 0 && i + N <= vocab) {
+#pragma unroll
+            for (int q = 0; q < N / 4; ++q) {
+                Row4 y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y.x[e] = p[4 * q + e];
+                *reinterpret_cast<Row4 *>(out + i + 4 * q) = y;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (i + e >= 0 && i + e < vocab) out[i + e] = p[e];
+        }
+    }
+}
+
+// Vectors of a thread that hold a row, or 0: the row does not fit, and is read twice.
+int row_vectors(int64_t vocab, bool f32)
+{
+    const int64_t n = (vocab + 31 + RT * (f32 ? 4 : 8) - 1) / (RT * (f32 ? 4 : 8));
+    return n <= 2 ? 2 : n <= 4 ? 4 : n <= 8 ? 8 : n <= 13 ? 13 : n <= 16 ? 16 : 0;
+}
 int probs_chunks(int64_t rows, int64_t vocab)
 {
     const int64_t want = (512 + rows - 1) / std::max<int64_t>(rows, 1);
     return (int)std::max<int64_t>(1, std::min<int64_t>({want, (vocab + 4095) / 4096, 64}));
 }
+template <typename T, int NV>
+void launch_rows(const T *x, int64_t xs, float *p, int64_t ps, int64_t rows, int vocab, float c, hipStream_t s)
+{
+    hipLaunchKernelGGL((token_probs_row_kernel<T, NV>), dim3((unsigned)rows), dim3(RT), 0, s, x, xs, p, ps, vocab, c);
+}
 
 // ---- verification -------------------------------------------------------------------------------------------------------------
-constexpr int VT = 1024, VW = VT / 64;
-
 struct VerifyArgs {
     const float *target, *draft;      // [n][R][target_stride], [n][R - 1][draft_stride] or null
     int64_t target_stride, draft_stride;
@@ -167,18 +260,94 @@ struct VerifyArgs {
     int32_t vocab, max_rows;
 };
 
-// What token i weighs in the draw: p, or what the draft's probability leaves of it.  (A NaN weighs nothing.)
-struct Weights {
+// A query's drafts, judged by every wavefront for itself: lane j tests draft j + 1, one comparison in 64 bits, exact for 32-bit inputs (u q has
+// 48 bits).  And what token i weighs in the draw that follows: p, or what the draft's probability leaves of it.  (A NaN weighs nothing.)
+struct Draw {
+    int rows, accepted;
     const float *p, *q;
-    int one;                          // the refused draft where there are no draft probabilities
-    bool refused;
-    __device__ __forceinline__ double of(int i, float pi) const
+    int one;                          // the refused draft where there are no draft probabilities, else -1
+    __device__ __forceinline__ Draw(const VerifyArgs &a, int64_t n)
     {
-        const double x = pi;
-        const double y = !refused ? 0.0 : q ? (double)q[i] : (i == one ? 1.0 : 0.0);
-        return x > y ? x - y : 0.0;
+        const int R = a.max_rows, lane = threadIdx.x & 63;
+        rows = a.rows ? min(a.rows[n], R) : R;
+        bool stands = false;
+        int token = -1;
+        if (lane < rows - 1) {
+            token = a.tokens[n * R + lane + 1];
+            if (token >= 0 && token < a.vocab) {
+                const double x = a.target[(n * R + lane) * a.target_stride + token];
+                const double y = a.draft ? (double)a.draft[(n * (R - 1) + lane) * a.draft_stride + token] : 1.0;
+                stands = (double)a.uniform[n * R + lane] * y < x;
+            }
+        }
+        accepted = __builtin_ctzll(~__ballot(stands));          // (at most 15)
+        const bool refused = accepted + 1 < rows;
+        p = a.target + (n * R + accepted) * a.target_stride;
+        q = a.draft && refused ? a.draft + (n * (R - 1) + accepted) * a.draft_stride : nullptr;
+        one = refused && !a.draft ? __shfl(token, accepted) : -1;
     }
-    __device__ __forceinline__ double operator()(int i) const { return of(i, p[i]); }
+    __device__ __forceinline__ void target_alone()
+    {
+        q = nullptr;
+        one = -1;
+    }
+    __device__ __forceinline__ double of(int i, float x, float y) const { return fmax((double)x - (i == one ? 1.0 : (double)y), 0.0); }
+    __device__ __forceinline__ double operator()(int i) const { return of(i, p[i], q ? q[i] : 0.f); }
+    // the weights of `from` .. + 7, of those in front of hi
+    __device__ __forceinline__ void eight(int from, int hi, double (&x)[8]) const
+    {
+        if (from + 8 <= hi) {
+            const Row4 none = {{0.f, 0.f, 0.f, 0.f}};
+            Row4 a[2], b[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                a[k] = *reinterpret_cast<const Row4 *>(p + from + 4 * k);
+                b[k] = q ? *reinterpret_cast<const Row4 *>(q + from + 4 * k) : none;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = of(from + e, a[e >> 2].x[e & 3], b[e >> 2].x[e & 3]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = from + e < hi ? (*this)(from + e) : 0.0;
+        }
+    }
+    // the weights of [lo, hi), by N threads of which this is number t
+    template <int N>
+    __device__ __forceinline__ double sum(int lo, int hi, int t) const
+    {
+        return q ? sum_of<N, true>(lo, hi, t) : sum_of<N, false>(lo, hi, t);
+    }
+    template <int N, bool Q>
+    __device__ __forceinline__ double sum_of(int lo, int hi, int t) const
+    {
+        double s[4] = {0.0, 0.0, 0.0, 0.0};
+        auto four = [&](Row4 x, const Row4 &y, int at) __attribute__((always_inline)) {
+            if (!Q && (uint32_t)(one - at) < 4u) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (at + e == one) x.x[e] = fmaxf(x.x[e] - 1.f, 0.f);        // (a weight of more than one leaves what is over)
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] += Q ? fmax((double)x.x[e] - (double)y.x[e], 0.0) : (double)fmaxf(x.x[e], 0.f);
+        };
+        int i = lo + 4 * t;
+        for (; i + 12 * N + 4 <= hi; i += 16 * N) {          // four loads on their way at once
+            Row4 x[4], y[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                x[k] = *reinterpret_cast<const Row4 *>(p + i + 4 * k * N);
+                if (Q) y[k] = *reinterpret_cast<const Row4 *>(q + i + 4 * k * N);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) four(x[k], y[k], i + 4 * k * N);
+        }
+        for (; i + 4 <= hi; i += 4 * N) {
+            const Row4 x = *reinterpret_cast<const Row4 *>(p + i);
+            four(x, Q ? *reinterpret_cast<const Row4 *>(q + i) : x, i);
+        }
+        for (; i < hi; ++i) s[0] += (*this)(i);          // (one thread's, fewer than four)
+        return (s[0] + s[1]) + (s[2] + s[3]);
+    }
 };
 __device__ __forceinline__ double wave_sum(double x)
 {
@@ -186,132 +355,203 @@ __device__ __forceinline__ double wave_sum(double x)
     for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d);
     return x;
 }
-
-// One workgroup per query.  A draft's test is one comparison in 64 bits, exact for 32-bit inputs (u q has 48 bits).  The draw goes
-// down the row by sums of whole segments, in 64 bits: 1024 threads sum 16 segments, the segment that the random number falls into is summed in 16
-// pieces again, and one wavefront finds the token in the piece.
-__global__ void __launch_bounds__(VT) verify_kernel(const VerifyArgs a)
+__device__ __forceinline__ double wave_scan(double x)          // sums of lanes 0 .. own
 {
-    __shared__ double part[2][VW];
-    const int64_t n = blockIdx.x;
-    const int R = a.max_rows, V = a.vocab;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int rows = a.rows ? min(a.rows[n], R) : R;
-    if (rows < 1) {          // a query that took no part
-        if ((int)threadIdx.x < R) a.out[n * R + threadIdx.x] = -1;
-        if (threadIdx.x == 0) a.accepted[n] = 0;
-        return;
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const double y = __shfl_up(x, d);
+        if (lane >= d) x += y;
     }
-    // every wavefront for itself: lane j judges draft j + 1
-    bool stands = false;
-    int token = 0;
-    if (lane < rows - 1) {
-        token = a.tokens[n * R + lane + 1];
-        if (token >= 0 && token < V) {
-            const double p = a.target[(n * R + lane) * a.target_stride + token];
-            const double q = a.draft ? (double)a.draft[(n * (R - 1) + lane) * a.draft_stride + token] : 1.0;
-            stands = (double)a.uniform[n * R + lane] * q < p;
-        }
+    return x;
+}
+// Of n <= 64 parts in order: their sum, and the first that t falls into, or the last that weighs anything (-1: none does), with t
+// from that part's beginning.  Every wavefront for itself.
+struct Parts {
+    double x, scan, sum;
+    __device__ __forceinline__ Parts(const double *part, int n)
+    {
+        const int lane = threadIdx.x & 63;
+        x = lane < n ? part[lane] : 0.0;
+        scan = wave_scan(x);
+        sum = __shfl(scan, 63);
     }
-    const int acc = __builtin_ctzll(~__ballot(stands));          // (at most 15)
-    Weights w;
-    w.p = a.target + (n * R + acc) * a.target_stride;
-    w.refused = acc + 1 < rows;
-    w.q = a.draft && w.refused ? a.draft + (n * (R - 1) + acc) * a.draft_stride : nullptr;
-    w.one = __shfl(token, acc);
-    const double u = a.uniform[n * R + R - 1];
-
-    // segments of the row, one per wavefront; p's own sums beside them, for a draft that leaves nothing
-    const int seg = (V + VW - 1) / VW;
-    auto sums = [&](int lo, int hi, double &sw, double &sp) __attribute__((always_inline)) {
-        sw = sp = 0.0;
-        for (int i = lo + lane; i < hi; i += 64) {
-            const float p = w.p[i];
-            sw += w.of(i, p);
-            if (p > 0.f) sp += (double)p;
+    __device__ __forceinline__ int falls_into(double &t) const
+    {
+        const uint64_t some = __ballot(x > 0.0), hit = __ballot(x > 0.0 && scan > t);
+        if (!some) return -1;
+        const int which = hit ? __builtin_ctzll(hit) : 63 - __builtin_clzll(some);
+        t -= __shfl(scan - x, which);
+        return which;
+    }
+};
+// The token of [lo, hi) that t falls into, by a workgroup of N threads; part: N / 64 doubles.  Ranges of more than eight tokens a thread are
+// narrowed by the sums of N / 64 pieces first; then every thread holds eight neighbouring tokens.
+template <int N>
+__device__ __forceinline__ int token_at(const Draw &w, int lo, int hi, double t, double *part)
+{
+    __shared__ int found, last;
+    constexpr int W = N / 64;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    while (hi - lo > 8 * N) {
+        const int piece = ((hi - lo + W - 1) / W + 3) / 4 * 4, from = min(hi, lo + wave * piece);
+        const double s = wave_sum(w.sum<64>(from, min(hi, from + piece), lane));
+        __syncthreads();
+        if (lane == 0) part[wave] = s;
+        __syncthreads();
+        const int which = Parts(part, W).falls_into(t);
+        if (which < 0) return -1;
+        lo += which * piece;
+        hi = min(hi, lo + piece);
+    }
+    const int from = lo + 8 * tid;
+    double x[8];
+    w.eight(from, hi, x);
+    double mine = 0.0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mine += x[e];
+    const double scan = wave_scan(mine);
+    __syncthreads();
+    if (lane == 63) part[wave] = scan;
+    if (tid == 0) found = last = -1;
+    __syncthreads();
+    const double other = lane < W ? part[lane] : 0.0;
+    double run = scan - mine + __shfl(wave_scan(other) - other, wave);
+    if (mine > 0.0) {
+        const bool beyond = run + mine > t;
+        int at = -1, top = -1;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            run += x[e];
+            if (x[e] > 0.0) top = from + e;
+            if (x[e] > 0.0 && at < 0 && run > t) at = from + e;
         }
-        sw = wave_sum(sw);
-        sp = wave_sum(sp);
-    };
-    auto chosen = [&](double t, int &which, double &before) __attribute__((always_inline)) {      // first part that t falls into, or the last that weighs anything
-        double run = 0.0;
-        which = -1;
-        before = 0.0;
-        for (int k = 0; k < VW; ++k) {
-            const double x = part[0][k];
-            if (x > 0.0) {
-                which = k;
-                before = run;
-            }
-            run += x;
-            if (x > 0.0 && run > t) break;
-        }
-    };
-    double sw, sp;
-    sums(min(V, wave * seg), min(V, (wave + 1) * seg), sw, sp);
-    if (lane == 0) {
-        part[0][wave] = sw;
-        part[1][wave] = sp;
+        atomicMax(&last, top);                                                                // the last token that weighs anything
+        if (beyond) atomicMax(&found, 0x7fffffff - (at >= 0 ? at : top));                     // the first one beyond t
     }
     __syncthreads();
-    double total = 0.0, total_p = 0.0;
-    for (int k = 0; k < VW; ++k) {
-        total += part[0][k];
-        total_p += part[1][k];
+    return found >= 0 ? 0x7fffffff - found : last;
+}
+__device__ __forceinline__ void answer(const VerifyArgs &a, int64_t n, const Draw &w, int next)
+{
+    const int R = a.max_rows, t = threadIdx.x;
+    if (t < R) a.out[n * R + t] = w.rows < 1 ? -1 : t < w.accepted ? a.tokens[n * R + t + 1] : t == w.accepted ? next : -1;
+    if (t == 0) {
+        a.accepted[n] = w.rows < 1 ? 0 : w.accepted;
+        if (a.done && w.rows >= 1) a.done[n] += w.accepted + 1;
     }
-    if (!(total > 0.0)) {             // the draft's probabilities cover the target's everywhere: the target's
-        w.refused = false;
-        w.q = nullptr;
-        total = total_p;
+}
+
+// The draw goes down the row by sums in 64 bits, of parts that get smaller: the token is the first at which the running sum is beyond u times the whole.
+// Many queries: one workgroup a query.  16 wavefronts sum a segment each; the segment that u falls into is looked through token by token.
+constexpr int VT = 512, VW = VT / 64;
+__global__ void __launch_bounds__(VT, 4) verify_kernel(const VerifyArgs a)
+{
+    __shared__ double part[VW];
+    const int64_t n = blockIdx.x;
+    Draw w(a, n);
+    if (w.rows < 1) return answer(a, n, w, -1);          // a query that took no part
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), seg = ((a.vocab + VW - 1) / VW + 3) / 4 * 4;
+    auto sums = [&]() __attribute__((always_inline)) {
+        const int lo = min(a.vocab, wave * seg);
+        const double s = wave_sum(w.sum<64>(lo, min(a.vocab, lo + seg), lane));
+        if (lane == 0) part[wave] = s;
         __syncthreads();
-        if ((int)threadIdx.x < VW) part[0][threadIdx.x] = part[1][threadIdx.x];
+    };
+    sums();
+    Parts all(part, VW);
+    if (!(all.sum > 0.0)) {                              // the draft's probabilities cover the target's everywhere
+        w.target_alone();
         __syncthreads();
+        sums();
+        all = Parts(part, VW);
     }
-    double t = u * total, before;
-    int which;
-    chosen(t, which, before);
+    double t = (double)a.uniform[n * a.max_rows + a.max_rows - 1] * all.sum;
+    const int which = all.falls_into(t);
     int next = -1;
-    if (which >= 0) {
-        t -= before;
-        const int lo = which * seg, hi = min(V, lo + seg), piece = (seg + VW - 1) / VW;
-        const int plo = min(hi, lo + wave * piece);
-        double s2, unused;
-        sums(plo, min(hi, plo + piece), s2, unused);
-        __syncthreads();
-        if (lane == 0) part[0][wave] = s2;
-        __syncthreads();
-        chosen(t, which, before);
-        t -= before;
-        if (wave == 0 && which >= 0) {
-            const int qlo = min(hi, lo + which * piece), qhi = min(hi, qlo + piece);
-            double run = 0.0;
-            for (int i0 = qlo; i0 < qhi; i0 += 64) {
-                const int i = i0 + lane;
-                const double x = i < qhi ? w(i) : 0.0;
-                double c = x;
+    if (which >= 0) next = token_at<VT>(w, which * seg, min(a.vocab, (which + 1) * seg), t, part);
+    answer(a, n, w, next);
+}
+// Few queries: `chunks` workgroups sum a query's row, a piece per wavefront, and one wavefront, in a launch of its own, looks through the
+// piece that u falls into.  (A workgroup there, with its barriers, took 8.8 us for a vocabulary of 131072.)
+constexpr int CW = 4, CT = 64 * CW, kMostChunks = 64;
+__device__ __forceinline__ int piece_length(int vocab, int chunks) { return ((vocab + chunks * CW - 1) / (chunks * CW) + 3) / 4 * 4; }
+__global__ void __launch_bounds__(CT) verify_sum_kernel(const VerifyArgs a, double *sums)
+{
+    const int64_t n = blockIdx.y;
+    const Draw w(a, n);
+    const int per = piece_length(a.vocab, (int)gridDim.x), k = (int)blockIdx.x * CW + ((int)threadIdx.x >> 6);
+    const int lo = (int)min<int64_t>(a.vocab, (int64_t)k * per), hi = (int)min<int64_t>(a.vocab, (int64_t)lo + per);
+    const double s = w.rows < 1 ? 0.0 : wave_sum(w.sum<64>(lo, hi, threadIdx.x & 63));
+    if ((threadIdx.x & 63) == 0) sums[n * (gridDim.x * CW) + k] = s;
+}
+__global__ void __launch_bounds__(64) verify_pick_kernel(const VerifyArgs a, const double *sums, int chunks)
+{
+    const int64_t n = blockIdx.x;
+    const int lane = threadIdx.x, pieces = chunks * CW;
+    double x[CW];                                        // pieces CW lane .. + CW - 1
 #pragma unroll
-                for (int d = 1; d < 64; d <<= 1) {
-                    const double y = __shfl_up(c, d);
-                    if (lane >= d) c += y;
-                }
-                const uint64_t hit = __ballot(x > 0.0 && run + c > t), some = __ballot(x > 0.0);
-                if (hit) {
-                    next = i0 + __builtin_ctzll(hit);
-                    break;
-                }
-                if (some) next = i0 + 63 - __builtin_clzll(some);
-                run += __shfl(c, 63);
+    for (int e = 0; e < CW; ++e) x[e] = CW * lane + e < pieces ? sums[n * pieces + CW * lane + e] : 0.0;
+    const double u = a.uniform[n * a.max_rows + a.max_rows - 1];
+    Draw w(a, n);
+    if (w.rows < 1) return answer(a, n, w, -1);
+    const int per = piece_length(a.vocab, chunks);
+    // of each lane's neighbouring weights x[], the one that t falls into; false: nothing weighs anything
+    double t;
+    int which_lane, which;
+    auto falls_into = [&](auto &v, auto scale) __attribute__((always_inline)) -> bool {
+        constexpr int E = sizeof(v) / sizeof(double);
+        double mine = 0.0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) mine += v[e];
+        const double scan = wave_scan(mine);
+        if (decltype(scale)::value) t = u * __shfl(scan, 63);
+        const uint64_t some = __ballot(mine > 0.0), hit = __ballot(mine > 0.0 && scan > t);
+        if (!some) return false;
+        which_lane = hit ? __builtin_ctzll(hit) : 63 - __builtin_clzll(some);
+        double run = scan - mine, before = 0.0;
+        int at = -1;
+        bool beyond = false;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            if (v[e] > 0.0 && !beyond) {
+                at = e;
+                before = run;
             }
+            run += v[e];
+            beyond = beyond || (v[e] > 0.0 && run > t);
         }
-    }
-    if (wave == 0) {
-        const int ahead = lane + 1 < R ? a.tokens[n * R + lane + 1] : 0;
-        if (lane < R) a.out[n * R + lane] = lane < acc ? ahead : lane == acc ? next : -1;
-        if (lane == 0) {
-            a.accepted[n] = acc;
-            if (a.done) a.done[n] += acc + 1;
+        which = __shfl(at, which_lane);
+        t -= __shfl(before, which_lane);
+        return true;
+    };
+    if (!falls_into(x, std::true_type{})) {              // the draft's probabilities cover the target's everywhere: all of the row again
+        w.target_alone();
+        for (int k = 0; k < pieces; ++k) {
+            const int lo = (int)min<int64_t>(a.vocab, (int64_t)k * per);
+            const double s = wave_sum(w.sum<64>(lo, (int)min<int64_t>(a.vocab, (int64_t)lo + per), lane));
+#pragma unroll
+            for (int e = 0; e < CW; ++e)
+                if (k == CW * lane + e) x[e] = s;
         }
+        if (!falls_into(x, std::true_type{})) return answer(a, n, w, -1);
     }
+    int lo = (CW * which_lane + which) * per, hi = min(a.vocab, lo + per), next = -1;
+    while (hi - lo > 512) {                              // a piece of more than eight tokens a lane is narrowed first
+        const int each = ((hi - lo + 63) / 64 + 3) / 4 * 4, from = min(hi, lo + lane * each);
+        double s[1] = {w.sum<1>(from, min(hi, from + each), 0)};
+        if (!falls_into(s, std::false_type{})) return answer(a, n, w, -1);
+        lo += which_lane * each;
+        hi = min(hi, lo + each);
+    }
+    double v[8];
+    w.eight(lo + 8 * lane, hi, v);
+    if (falls_into(v, std::false_type{})) next = lo + 8 * which_lane + which;
+    answer(a, n, w, next);
+}
+int verify_chunks(int64_t n, int64_t vocab)
+{
+    return (int)std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(n, 1), (vocab + 2047) / 2048, (int64_t)kMostChunks}));
 }
 
 }  // namespace
@@ -354,7 +594,18 @@ int sgc_token_probs(sgc_ctx *ctx, int64_t n_rows, int32_t vocab, const void *dev
         const T *x = static_cast<const T *>(dev_logits) + first * logits_stride;
         float *p = dev_probs + first * probs_stride;
         const dim3 grid((unsigned)chunks, (unsigned)rows);
-        if (chunks == 1) {
+        const int nv = chunks == 1 ? row_vectors(vocab, logits_dtype == SGC_F32) : 0;
+        if (nv == 2) {
+            launch_rows<T, 2>(x, logits_stride, p, probs_stride, rows, vocab, c, s);
+        } else if (nv == 4) {
+            launch_rows<T, 4>(x, logits_stride, p, probs_stride, rows, vocab, c, s);
+        } else if (nv == 8) {
+            launch_rows<T, 8>(x, logits_stride, p, probs_stride, rows, vocab, c, s);
+        } else if (nv == 13) {
+            launch_rows<T, 13>(x, logits_stride, p, probs_stride, rows, vocab, c, s);
+        } else if (nv == 16) {
+            launch_rows<T, 16>(x, logits_stride, p, probs_stride, rows, vocab, c, s);
+        } else if (chunks == 1) {
             hipLaunchKernelGGL((token_probs_kernel<T, true, true>), grid, dim3(PT), 0, s, x, logits_stride, p, probs_stride, vocab, c, nullptr, 1);
         } else {
             hipLaunchKernelGGL((token_probs_kernel<T, true, false>), grid, dim3(PT), 0, s, x, logits_stride, p, probs_stride, vocab, c, parts + first * chunks, chunks);
@@ -375,9 +626,9 @@ int sgc_token_probs(sgc_ctx *ctx, int64_t n_rows, int32_t vocab, const void *dev
 
 size_t sgc_verify_workspace(int32_t n_queries, int32_t vocab)
 {
-    (void)n_queries;
-    (void)vocab;
-    return 0;
+    if (n_queries <= 0 || vocab <= 0) return 0;
+    const int chunks = verify_chunks(n_queries, vocab);
+    return chunks > 1 ? (size_t)n_queries * chunks * CW * sizeof(double) : 0;
 }
 
 int sgc_verify_drafts(sgc_ctx *ctx, int32_t n_queries, int32_t max_rows, int32_t vocab, const float *dev_target, int64_t target_stride, const float *dev_draft,
@@ -411,7 +662,15 @@ int sgc_verify_drafts(sgc_ctx *ctx, int32_t n_queries, int32_t max_rows, int32_t
     v.done = dev_done;
     v.vocab = vocab;
     v.max_rows = max_rows;
-    hipLaunchKernelGGL(verify_kernel, dim3((unsigned)n_queries), dim3(VT), 0, static_cast<hipStream_t>(hip_stream), v);
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    if (need > 0) {
+        const int chunks = verify_chunks(n_queries, vocab);
+        double *sums = static_cast<double *>(dev_workspace);
+        hipLaunchKernelGGL(verify_sum_kernel, dim3((unsigned)chunks, (unsigned)n_queries), dim3(CT), 0, s, v, sums);
+        hipLaunchKernelGGL(verify_pick_kernel, dim3((unsigned)n_queries), dim3(64), 0, s, v, sums, chunks);
+    } else {
+        hipLaunchKernelGGL(verify_kernel, dim3((unsigned)n_queries), dim3(VT), 0, s, v);
+    }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return report(ctx, SGC_EHIP, "verify_kernel: %s", hipGetErrorString(e));
     return SGC_OK;
