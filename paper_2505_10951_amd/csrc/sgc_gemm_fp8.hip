@@ -220,7 +220,7 @@ __device__ __forceinline__ i32x8 join(const u32x4 &a, const u32x4 &b)
     return i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
 }
 
-// acc += w x^T over 64 codes ...
+// acc += w x^T over 64 codes
 template <int NBL, int MBL>
 __device__ __forceinline__ void products(const i32x8 (&w)[NBL], const i32x8 (&x)[MBL], int we, const int (&xe)[MBL], f32x16 (&acc)[NBL][MBL])
 {
@@ -228,14 +228,6 @@ __device__ __forceinline__ void products(const i32x8 (&w)[NBL], const i32x8 (&x)
     for (int i = 0; i < NBL; ++i)
 #pragma unroll
         for (int j = 0; j < MBL; ++j) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w[i], x[j], acc[i][j], 0, 0, 0, we, 0, xe[j]);
-}
-// ... and over eight of a lane's 32 (two words of codes, the same ones of the widened rows)
-template <int MBL>
-__device__ __forceinline__ void products16(uint32_t w0, uint32_t w1, float we, const bf16x8 (&x)[MBL], f32x16 (&acc)[1][MBL])
-{
-    const bf16x8 w = widen8(w0, w1, we);
-#pragma unroll
-    for (int j = 0; j < MBL; ++j) acc[0][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, x[j], acc[0][j], 0, 0, 0);
 }
 // The chunk of 16 bytes (eight widened elements) of a 64-element half that belongs to words 2 t, 2 t + 1 of a lane's operand
 __device__ __forceinline__ int wide_chunk(int t, int h) { return (t >> 1) * 4 + h * 2 + (t & 1); }
@@ -287,7 +279,7 @@ __device__ __forceinline__ void store_block(const Fp8Args &a, const f32x16 &acc,
     }
 }
 
-// ---- many rows: tiles through LDS ------------------------------------------------------------------------------------------
+// ---- tiles through LDS ------------------------------------------------------------------------------------------
 // A step is one block of 128 codes: slabs of TM rows of x and TN rows of W, 128 bytes each, the eight 16-byte chunks of a row permuted by
 // (row & 7) ^ ((row >> 3) & 1) on the global side of the copy, so that 16 consecutive rows' reads of a chunk cover all banks.
 // Four wavefronts, each a quarter of the tile.  Workgroup b runs on XCD b % 8; an XCD takes a contiguous run of tiles that walks groups of
@@ -309,19 +301,22 @@ __device__ __forceinline__ TileAt tile_at(const Fp8Args &a)
     return t;
 }
 
-template <int TM_, int TN_, int NST_, int WGS_>
-struct MidTile {
-    static constexpr int TM = TM_, TN = TN_, NST = NST_, WGS = WGS_;
-    static constexpr int A_BYTES = TM * BLK, B_BYTES = TN * BLK, STAGE = A_BYTES + B_BYTES;
-    static constexpr int COPIES = STAGE / 4096, A_COPIES = A_BYTES / 4096;
+template <int TM_, int TN_, int NST_, bool F32_, bool TURN_ = false>
+struct Tile {
+    static constexpr int TM = TM_, TN = TN_, NST = NST_;
+    static constexpr bool F32 = F32_, TURN = TURN_;
+    static constexpr int XS = F32 ? 2 : 1;                               // slabs of x a step: widened rows are 256 bytes a block
+    static constexpr int X_SLAB = TM * BLK, X_BYTES = XS * X_SLAB, W_BYTES = TN * BLK, STAGE = X_BYTES + W_BYTES;
+    static constexpr int COPIES = STAGE / 4096, X_COPIES = X_BYTES / 4096;      // 1 KiB copies of a wavefront
     static constexpr int LDS = NST * STAGE;
     static constexpr int MBL = TM / 64, NBL = TN / 64;
 };
 
 template <class T>
-__global__ void __launch_bounds__(256, T::WGS) project_fp8_tile_kernel(const Fp8Args a)
+__global__ void __launch_bounds__(256, 1) project_fp8_tile_kernel(const Fp8Args a)
 {
     constexpr int MBL = T::MBL, NBL = T::NBL, NST = T::NST;
+    static_assert(NST >= 2 && T::COPIES * (NST - 1) < 64 && T::LDS <= 160 * 1024, "copies in flight are counted in 6 bits");
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wm = wave >> 1, wn = wave & 1, h = lane >> 5, l31 = lane & 31;
@@ -329,25 +324,32 @@ __global__ void __launch_bounds__(256, T::WGS) project_fp8_tile_kernel(const Fp8
     if (t.none) return;
     const int64_t m0 = (int64_t)t.rt * T::TM;
     const int n0 = t.ct * T::TN, rows = (int)min<int64_t>(T::TM, a.M - m0), cols = min(T::TN, a.N - n0);
-    const uint32_t ld = (uint32_t)a.KB * BLK;
+    const uint32_t ld = (uint32_t)a.KB * BLK, ldx = ld * T::XS;
     const int KB4 = (a.KB + 3) / 4;
+    // Step i multiplies block block_of(i).  TURN: tiles of different columns begin at blocks of their own, since rows of W that lie a power
+    // of two apart, all asked for at the same block, meet in few memory channels (64 x 50021 x 4096 58.8 us that way, 50.5 turned; over 4224 codes 51.8).
+    const int first = T::TURN && a.KB % 4 == 0 ? t.ct * 4 % a.KB : 0;
+    auto block_of = [&](int i) __attribute__((always_inline)) { return !T::TURN || i + first < a.KB ? i + first : i + first - a.KB; };
 
     // copies: a wavefront's instruction moves 8 rows; lane (lr, slot) fetches chunk slot ^ perm(row); rows past the end repeat the last
     const int lr = lane >> 3, slot = lane & 7;
-    const Operand x_op = operand(a.ws.codes + m0 * ld, (uint32_t)rows * ld), w_op = operand(a.w + (int64_t)n0 * ld, (uint32_t)cols * ld);
+    const Operand x_op = operand(T::F32 ? reinterpret_cast<const char *>(a.ws.wide) + m0 * ldx : reinterpret_cast<const char *>(a.ws.codes) + m0 * ldx, (uint32_t)rows * ldx);
+    const Operand w_op = operand(a.w + (int64_t)n0 * ld, (uint32_t)cols * ld);
     uint32_t off[T::COPIES];
 #pragma unroll
     for (int i = 0; i < T::COPIES; ++i) {
-        const bool is_x = i < T::A_COPIES;
-        const int row = is_x ? (T::TM / 4) * wave + 8 * i + lr : (T::TN / 4) * wave + 8 * (i - T::A_COPIES) + lr;
-        off[i] = (uint32_t)min(row, (is_x ? rows : cols) - 1) * ld + (uint32_t)(slot ^ lr ^ ((row >> 3) & 1)) * 16;
+        const bool is_x = i < T::X_COPIES;
+        const int c = is_x ? wave * T::X_COPIES + i : wave * (T::COPIES - T::X_COPIES) + i - T::X_COPIES;      // the copy's number in its part of the stage
+        const int sub = is_x ? c / (T::TM / 8) : 0, row = 8 * (is_x ? c % (T::TM / 8) : c) + lr;
+        off[i] = (uint32_t)min(row, (is_x ? rows : cols) - 1) * (is_x ? ldx : ld) + sub * BLK + (uint32_t)(slot ^ lr ^ ((row >> 3) & 1)) * 16;
     }
-    auto issue = [&](int kt, int stage) __attribute__((always_inline)) {
+    auto issue = [&](int i0, int stage) __attribute__((always_inline)) {
         char *st = smem + stage * T::STAGE;
+        const uint32_t k = (uint32_t)block_of(i0) * BLK;
 #pragma unroll
         for (int i = 0; i < T::COPIES; ++i)
-            copy_1k_to_lds(i < T::A_COPIES ? x_op : w_op, off[i], (uint32_t)kt * BLK,
-                           st + (i < T::A_COPIES ? wave * (T::A_BYTES / 4) + i * 1024 : T::A_BYTES + wave * (T::B_BYTES / 4) + (i - T::A_COPIES) * 1024));
+            copy_1k_to_lds(i < T::X_COPIES ? x_op : w_op, off[i], i < T::X_COPIES ? k * T::XS : k,
+                           st + (i < T::X_COPIES ? (wave * T::X_COPIES + i) * 1024 : T::X_BYTES + (wave * (T::COPIES - T::X_COPIES) + i - T::X_COPIES) * 1024));
     };
     f32x16 acc[NBL][MBL];
 #pragma unroll
@@ -357,102 +359,124 @@ __global__ void __launch_bounds__(256, T::WGS) project_fp8_tile_kernel(const Fp8
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
-    // operand reads: lane (l31, h) reads chunks 2 kk + h of its row, kk = 2 s and 2 s + 1 for the 64-code operand s
-    uint32_t r_off[4];
-#pragma unroll
-    for (int kk = 0; kk < 4; ++kk) r_off[kk] = (uint32_t)l31 * BLK + (((uint32_t)kk * 32) ^ ((uint32_t)(h ^ (lane & 7) ^ ((lane >> 3) & 1)) * 16));
-    const uint32_t x_region = (uint32_t)wm * (T::A_BYTES / 2), w_region = T::A_BYTES + (uint32_t)wn * (T::B_BYTES / 2);
-    auto load_ops = [&](int stage, i32x8 (&x)[2][MBL], i32x8 (&w)[2][NBL]) __attribute__((always_inline)) {
-        const char *st = smem + stage * T::STAGE;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-#pragma unroll
-            for (int j = 0; j < MBL; ++j) {
-                const char *p = st + x_region + j * 4096;
-                x[s][j] = join(*reinterpret_cast<const u32x4 *>(p + r_off[2 * s]), *reinterpret_cast<const u32x4 *>(p + r_off[2 * s + 1]));
-            }
-#pragma unroll
-            for (int i = 0; i < NBL; ++i) {
-                const char *p = st + w_region + i * 4096;
-                w[s][i] = join(*reinterpret_cast<const u32x4 *>(p + r_off[2 * s]), *reinterpret_cast<const u32x4 *>(p + r_off[2 * s + 1]));
-            }
-        }
+    // operand reads: lane (l31, h) reads chunks 2 kk + h of its row, kk = 2 s and 2 s + 1 for the 64-code operand s; of widened rows
+    // the chunks that hold the same elements
+    const uint32_t perm = (uint32_t)((lane & 7) ^ ((lane >> 3) & 1)), row_off = (uint32_t)l31 * BLK;
+    struct Operands {
+        u32x4 w[4][NBL], x[T::F32 ? 8 : 4][MBL];
     };
-    // scales: words of four steps
+    auto load_ops = [&](int stage, Operands &o) __attribute__((always_inline)) {
+        const char *xs = smem + stage * T::STAGE + (uint32_t)wm * (T::X_SLAB / 2) + row_off;
+        const char *wsl = smem + stage * T::STAGE + T::X_BYTES + (uint32_t)wn * (T::W_BYTES / 2) + row_off;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+            for (int i = 0; i < NBL; ++i) o.w[kk][i] = *reinterpret_cast<const u32x4 *>(wsl + i * 4096 + ((uint32_t)(2 * kk + h) ^ perm) * 16);
+#pragma unroll
+        for (int q = 0; q < (T::F32 ? 8 : 4); ++q)
+#pragma unroll
+            for (int j = 0; j < MBL; ++j)
+                o.x[q][j] = *reinterpret_cast<const u32x4 *>(xs + (T::F32 ? (q >> 2) * T::X_SLAB : 0) + j * 4096 + ((uint32_t)(T::F32 ? wide_chunk(q & 3, h) : 2 * q + h) ^ perm) * 16);
+    };
+    // scales: words of four blocks
     const uint32_t *xe_at = a.ws.xe + m0;
-    const uint32_t *we_at = a.ws.we + (int64_t)((n0 + wn * (T::TN / 2)) / BLK) * KB4;       // (past the end in a wavefront without columns: clamped)
     const bool some = n0 + wn * (T::TN / 2) < a.N;
-    if (!some) we_at = a.ws.we;
+    const uint32_t *we_at = a.ws.we + (int64_t)(some ? (n0 + wn * (T::TN / 2)) / BLK : 0) * KB4;
     int at[MBL];
 #pragma unroll
     for (int j = 0; j < MBL; ++j) at[j] = min(wm * (T::TM / 2) + 32 * j + l31, rows - 1);
-    uint32_t xw[MBL], xw_next[MBL], ww = uniform_word(we_at), ww_next = ww;
+    uint32_t xw[MBL], xw_next[MBL], ww = uniform_word(we_at + first / 4), ww_next = ww;
 #pragma unroll
-    for (int j = 0; j < MBL; ++j) xw_next[j] = xw[j] = xe_at[at[j]];
+    for (int j = 0; j < MBL; ++j) xw_next[j] = xw[j] = T::F32 ? 0 : xe_at[(int64_t)(first / 4) * a.M + at[j]];
 
     int stage = 0;
     auto after = [&](int s) __attribute__((always_inline)) { return s == NST - 1 ? 0 : s + 1; };
-    auto step = [&](int kt, const i32x8 (&x)[2][MBL], const i32x8 (&w)[2][NBL], i32x8 (&xn)[2][MBL], i32x8 (&wn_)[2][NBL], auto steady) __attribute__((always_inline)) {
+    auto step = [&](int i, const Operands &o, Operands &next, auto steady) __attribute__((always_inline)) {
         constexpr bool STEADY = decltype(steady)::value;
-        if (STEADY || kt + NST <= a.KB)
+        if (STEADY || i + NST <= a.KB)
             step_barrier<(NST - 2) * T::COPIES>();
         else
             step_barrier<0>();
         const int mine = stage;
         stage = after(stage);
-        if (!STEADY && kt + NST < a.KB) issue(kt + NST, mine);
-        load_ops(stage, xn, wn_);          // (behind the last step: some old step's operands, never used)
-        if (STEADY) issue(kt + NST, mine);
-        int xe[MBL];
-        const int sh = 8 * (kt & 3);
+        if (!STEADY && i + NST < a.KB) issue(i + NST, mine);
+        load_ops(stage, next);             // (behind the last step: some old step's operands, never used)
+        if (STEADY) issue(i + NST, mine);
+        const int sh = 8 * (i & 3), we = (int)((ww >> sh) & 0xFF);
+        if constexpr (T::F32) {
 #pragma unroll
-        for (int j = 0; j < MBL; ++j) xe[j] = (int)((xw[j] >> sh) & 0xFF);
-        const int we = (int)((ww >> sh) & 0xFF);
+            for (int q = 0; q < 8; ++q)
 #pragma unroll
-        for (int s = 0; s < 2; ++s) products(w[s], x[s], we, xe, acc);
+                for (int n = 0; n < NBL; ++n) {
+                    const bf16x8 w = widen8(o.w[q >> 1][n][2 * (q & 1)], o.w[q >> 1][n][2 * (q & 1) + 1], scale_of(we));
+#pragma unroll
+                    for (int j = 0; j < MBL; ++j) acc[n][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, __builtin_bit_cast(bf16x8, o.x[q][j]), acc[n][j], 0, 0, 0);
+                }
+        } else {
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int n = 0; n < NBL; ++n)
+#pragma unroll
+                    for (int j = 0; j < MBL; ++j)
+                        acc[n][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(join(o.w[2 * s][n], o.w[2 * s + 1][n]), join(o.x[2 * s][j], o.x[2 * s + 1][j]), acc[n][j], 0, 0, 0,
+                                                                                    we, 0, (int)((xw[j] >> sh) & 0xFF));
+        }
+        if (STEADY) {          // reads under the first half of the products, copies under the second (a copy may not pass a read of LDS)
+            constexpr int HALF = (T::F32 ? 4 : 1) * NBL * MBL, R = 4 * NBL + (T::F32 ? 8 : 4) * MBL, READS = (R + HALF - 1) / HALF, COPIES = (T::COPIES + HALF - 1) / HALF;
+#pragma unroll
+            for (int k = 0; k < HALF; ++k) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+            }
+#pragma unroll
+            for (int k = 0; k < HALF; ++k) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x010, COPIES, 0);
+            }
+        }
         __builtin_amdgcn_sched_barrier(0);
     };
-    // scales of the four steps from kt on; the words of the four behind them are on their way from here (asked for unconditionally:
-    // behind a branch the compiler waits for them, and for every copy in flight, at once: 1280 x 4096 x 4096 49.8 us)
-    auto scales = [&](int kt) __attribute__((always_inline)) {
-        const int next = min(kt / 4 + 1, KB4 - 1);
+    // Scales of the four steps from i on; the words of the four behind them are on their way from here (asked for unconditionally:
+    // behind a branch the compiler waits for them, and for every copy in flight, at once: 1280 x 4096 x 4096 46.4 us, now 41.4).
+    auto scales = [&](int i) __attribute__((always_inline)) {
+        const int next = block_of(min(i + 4, a.KB - 1)) / 4;
 #pragma unroll
         for (int j = 0; j < MBL; ++j) {
             xw[j] = xw_next[j];
-            xw_next[j] = xe_at[(int64_t)next * a.M + at[j]];
+            if (!T::F32) xw_next[j] = xe_at[(int64_t)next * a.M + at[j]];
         }
         ww = ww_next;
         ww_next = uniform_word(we_at + next);
     };
+    __builtin_amdgcn_sched_barrier(0);
+    // (of short rows the last block again: with copies behind branches the compiler loses count of them, and every wait for scales waits for all)
 #pragma unroll
-    for (int i = 0; i < NST; ++i)
-        if (i < a.KB) issue(i, i);
-    i32x8 x0[2][MBL], w0[2][NBL], x1[2][MBL], w1[2][NBL];
-    if (a.KB >= NST)
-        step_barrier<(NST - 1) * T::COPIES>();
-    else
-        step_barrier<0>();
-    load_ops(0, x0, w0);
-    int kt = 0;
-    for (; kt + 3 + NST < a.KB; kt += 4) {
-        scales(kt);
-        step(kt, x0, w0, x1, w1, std::true_type{});
-        step(kt + 1, x1, w1, x0, w0, std::true_type{});
-        step(kt + 2, x0, w0, x1, w1, std::true_type{});
-        step(kt + 3, x1, w1, x0, w0, std::true_type{});
+    for (int i = 0; i < NST; ++i) issue(min(i, a.KB - 1), i);
+    Operands o0, o1;
+    step_barrier<(NST - 1) * T::COPIES>();
+    load_ops(0, o0);
+    int i = 0;
+    for (; i + 3 + NST < a.KB; i += 4) {
+        scales(i);
+        step(i, o0, o1, std::true_type{});
+        step(i + 1, o1, o0, std::true_type{});
+        step(i + 2, o0, o1, std::true_type{});
+        step(i + 3, o1, o0, std::true_type{});
     }
-    for (; kt < a.KB; kt += 2) {
-        if ((kt & 3) == 0) scales(kt);
-        step(kt, x0, w0, x1, w1, std::false_type{});
-        if (kt + 1 < a.KB) step(kt + 1, x1, w1, x0, w0, std::false_type{});
+    for (; i < a.KB; i += 2) {
+        if ((i & 3) == 0) scales(i);
+        step(i, o0, o1, std::false_type{});
+        if (i + 1 < a.KB) step(i + 1, o1, o0, std::false_type{});
     }
+    step_barrier<0>();          // (no copy may arrive in LDS that is somebody else's)
     if (!some) return;
 #pragma unroll
     for (int j = 0; j < MBL; ++j)
 #pragma unroll
-        for (int i = 0; i < NBL; ++i) {
-            const int n = n0 + wn * (T::TN / 2) + 32 * i;
-            if (n < a.N) store_block<false>(a, acc[i][j], m0 + wm * (T::TM / 2) + 32 * j + l31, n, h);
+        for (int n = 0; n < NBL; ++n) {
+            const int at_n = n0 + wn * (T::TN / 2) + 32 * n;
+            if (at_n < a.N) store_block<T::F32>(a, acc[n][j], m0 + wm * (T::TM / 2) + 32 * j + l31, at_n, h);
         }
 }
 
@@ -506,13 +530,14 @@ __global__ void __launch_bounds__(256, 1) project_fp8_big_kernel(const Fp8Args a
             x[b] = join(*reinterpret_cast<const u32x4 *>(xs + b * 4096 + r_off[2 * s]), *reinterpret_cast<const u32x4 *>(xs + b * 4096 + r_off[2 * s + 1]));
         }
     };
-    // issue order of half a step: 16 products, the next half's 16 reads under the first eight, eight copies between all
+    // issue order of half a step: 16 products, the next half's 16 reads under the first eight, eight copies under the others (a copy may
+    // not pass a read of LDS: dealt over all products the order could not be had, and the compiler issued all of them at once)
     auto order = [&](auto reads, auto copies) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             if (decltype(reads)::value && i < 8) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-            if (decltype(copies)::value && (i & 1)) __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
+            if (decltype(copies)::value && i >= 8) __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
     };
@@ -586,286 +611,8 @@ __global__ void __launch_bounds__(256, 1) project_fp8_big_kernel(const Fp8Args a
         }
 }
 
-// ---- few rows: W's bytes ----------------------------------------------------------------------------------------------------
-// W goes straight from memory to registers, two blocks of 128 ahead.
-struct WeightRows {
-    const uint8_t *at;
-    int last;
-    __device__ __forceinline__ WeightRows(const Fp8Args &a, int n0, int l31, int h) : at(a.w + (int64_t)min(n0 + l31, a.N - 1) * a.KB * BLK + h * 16), last(a.KB - 1) {}
-    __device__ __forceinline__ void load(int kb, u32x4 (&c)[4]) const
-    {
-        const uint8_t *p = at + (int64_t)min(kb, last) * BLK;
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) c[kk] = *reinterpret_cast<const u32x4 *>(p + kk * 32);
-    }
-};
-
-// Few features: a workgroup takes 32 of them and all rows (up to 32 MBL); its eight wavefronts take every eighth block of 128 codes and add
-// up through LDS.  W and x of a block are asked for RING - 1 blocks ahead.
-// RAW: bf16 x is quantised here, in registers, by every workgroup for itself: a launch less (20 x 6144 x 4096: 12.5 us with it).
-struct FewX {
-    const uint16_t *x;            // RAW: rows of x, their distance and length, and W's exponents as the caller has them
-    int64_t stride;
-    int32_t K;
-    const uint8_t *wexps;
-};
-typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-typedef __attribute__((ext_vector_type(2))) short s16x2;
-constexpr int FW = 8;
-template <int MBL, bool F32, bool RAW, int RING>
-__global__ void __launch_bounds__(FW * 64, 2) project_fp8_few_kernel(const Fp8Args a, const FewX fx)
-{
-    extern __shared__ __attribute__((aligned(16))) float part[];          // [FW / 2][MBL][16][64]
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5, l31 = lane & 31;
-    const int n0 = (int)blockIdx.x * 32, KB4 = (a.KB + 3) / 4;
-    const int M = (int)a.M;
-    const WeightRows w_rows(a, n0, l31, h);
-    int row[MBL];
-#pragma unroll
-    for (int j = 0; j < MBL; ++j) row[j] = min(32 * j + l31, M - 1);
-    f32x16 acc[1][MBL];
-#pragma unroll
-    for (int j = 0; j < MBL; ++j)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[0][j][r] = 0.f;
-    constexpr int XR = F32 || RAW ? 8 : 4;          // 16-byte pieces of a lane's share of a row
-    struct Block {
-        u32x4 w[4], x[MBL][XR];
-        int we, xe[MBL];
-    };
-    auto load = [&](int kb, Block &b) __attribute__((always_inline)) {
-        const int kc = min(kb, a.KB - 1);
-        w_rows.load(kc, b.w);
-        if (RAW)
-            b.we = fx.wexps[(int64_t)(n0 / BLK) * a.KB + kc];
-        else
-            b.we = (int)((a.ws.we[(int64_t)(n0 / BLK) * KB4 + kc / 4] >> (8 * (kc & 3))) & 0xFF);
-#pragma unroll
-        for (int j = 0; j < MBL; ++j) {
-            if (!F32 && !RAW) b.xe[j] = (int)((a.ws.xe[(int64_t)(kc / 4) * M + row[j]] >> (8 * (kc & 3))) & 0xFF);
-#pragma unroll
-            for (int i = 0; i < XR; ++i) {
-                if (RAW) {
-                    const int k = kc * BLK + (i >> 1) * 32 + h * 16;          // (16 elements of a row are there or not as a whole)
-                    b.x[j][i] = k < fx.K ? *reinterpret_cast<const u32x4 *>(fx.x + row[j] * fx.stride + k + (i & 1) * 8) : u32x4{0, 0, 0, 0};
-                } else if (F32) {
-                    b.x[j][i] = *reinterpret_cast<const u32x4 *>(a.ws.wide + ((int64_t)row[j] * a.KB + kc) * BLK + (i >> 2) * 64 + wide_chunk(i & 3, h) * 8);
-                } else {
-                    b.x[j][i] = *reinterpret_cast<const u32x4 *>(a.ws.codes + ((int64_t)row[j] * a.KB + kc) * BLK + i * 32 + h * 16);
-                }
-            }
-        }
-    };
-    // RAW: the lane's 64 elements of a block as codes (16 words) and their exponent; the other 64 of the row are in the lane 32 away
-    auto quantise = [&](const u32x4 (&x)[XR], uint32_t (&code)[16]) __attribute__((always_inline)) -> int {
-        u16x2 top2 = {0, 0};
-#pragma unroll
-        for (int i = 0; i < XR; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) top2 = __builtin_elementwise_max(top2, __builtin_bit_cast(u16x2, x[i][e] & 0x7FFF7FFFu));
-        uint32_t top = max((uint32_t)top2[0], (uint32_t)top2[1]);
-        top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-        const bool odd = top >= 0x7F80u;
-        if (__any(odd)) {               // something is not finite: it does not count
-            top = 0;
-#pragma unroll
-            for (int i = 0; i < XR; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t lo = x[i][e] & 0x7FFFu, hi = (x[i][e] >> 16) & 0x7FFFu;
-                    top = max(top, max(lo < 0x7F80u ? lo : 0u, hi < 0x7F80u ? hi : 0u));
-                }
-            top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-        }
-        const int e8 = biased_exponent(top << 16);
-        const float scale = scale_of(e8);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            s16x2 c = {0, 0};
-            c = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c, __builtin_bit_cast(bf16x2, (uint32_t)x[i >> 1][2 * (i & 1)]), scale, false);
-            c = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c, __builtin_bit_cast(bf16x2, (uint32_t)x[i >> 1][2 * (i & 1) + 1]), scale, true);
-            code[i] = __builtin_bit_cast(uint32_t, c);
-        }
-        if (__any(odd)) {
-#pragma unroll
-            for (int i = 0; i < 64; ++i) {
-                const uint32_t b = (x[i >> 3][(i & 7) >> 1] >> (16 * (i & 1))) & 0x7FFFu;
-                if (b >= 0x7F80u) code[i >> 2] = (code[i >> 2] & ~(0xFFu << (8 * (i & 3)))) | 0x7Fu << (8 * (i & 3));
-            }
-        }
-        return e8;
-    };
-    auto multiply = [&](const Block &b) __attribute__((always_inline)) {
-        uint32_t code[MBL][16];
-        int xe[MBL];
-        if (RAW)
-#pragma unroll
-            for (int j = 0; j < MBL; ++j) xe[j] = quantise(b.x[j], code[j]);
-        const int we = __builtin_amdgcn_readfirstlane(b.we);
-        if constexpr (F32) {
-#pragma unroll
-            for (int t = 0; t < 8; ++t) {
-                bf16x8 x[MBL];
-#pragma unroll
-                for (int j = 0; j < MBL; ++j) {
-                    if (RAW)
-                        x[j] = widen8(code[j][2 * t], code[j][2 * t + 1], scale_of(xe[j]));
-                    else
-                        x[j] = __builtin_bit_cast(bf16x8, b.x[j][t % XR]);
-                }
-                products16(b.w[t >> 1][2 * (t & 1)], b.w[t >> 1][2 * (t & 1) + 1], scale_of(we), x, acc);
-            }
-        } else {
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                i32x8 x[MBL];
-                const i32x8 w[1] = {join(b.w[2 * s], b.w[2 * s + 1])};
-#pragma unroll
-                for (int j = 0; j < MBL; ++j) {
-                    if (RAW) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) x[j][i] = (int)code[j][8 * s + i];
-                    } else {
-                        x[j] = join(b.x[j][2 * s], b.x[j][2 * s + 1]);
-                        xe[j] = b.xe[j];
-                    }
-                }
-                products(w, x, we, xe, acc);
-            }
-        }
-    };
-    Block b[RING];
-#pragma unroll
-    for (int i = 0; i < RING - 1; ++i) load(wave + i * FW, b[i]);
-    for (int k0 = wave; k0 < a.KB; k0 += RING * FW) {
-#pragma unroll
-        for (int i = 0; i < RING; ++i) {
-            if (k0 + i * FW >= a.KB) break;
-            load(k0 + (i + RING - 1) * FW, b[(i + RING - 1) % RING]);
-            multiply(b[i]);
-        }
-    }
-    // the eight partial sums: the upper half of the wavefronts hand theirs to the lower, then half of those, ...
-#pragma unroll
-    for (int half = FW / 2; half >= 1; half >>= 1) {
-        float *mine = part + (wave & (half - 1)) * (MBL * 1024) + lane;
-        if (wave >= half && wave < 2 * half)
-#pragma unroll
-            for (int j = 0; j < MBL; ++j)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) mine[(j * 16 + r) * 64] = acc[0][j][r];
-        __syncthreads();
-        if (wave < half)
-#pragma unroll
-            for (int j = 0; j < MBL; ++j)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) acc[0][j][r] += mine[(j * 16 + r) * 64];
-        __syncthreads();
-    }
-    if (wave == 0)
-#pragma unroll
-        for (int j = 0; j < MBL; ++j) store_block<F32>(a, acc[0][j], 32 * j + l31, n0, h);
-}
-
-// Many features: four wavefronts of 32 features each share 32 MBL rows, whose blocks pass through LDS, in a ring of three (read by every
-// workgroup from L2 for 32 features, 64 rows were twice the bytes of W: 99 us for 64 x 50021 x 4096).
-template <int MBL, bool F32>
-__global__ void __launch_bounds__(256, 2) project_fp8_stream_kernel(const Fp8Args a)
-{
-    constexpr int XS = F32 ? 2 : 1, TM = 32 * MBL, SUB = TM * BLK, SLAB = XS * SUB, XC = MBL * XS, LOADS = 4 + XC + (F32 ? 0 : MBL);
-    extern __shared__ __attribute__((aligned(1024))) char smem[];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5, l31 = lane & 31;
-    const TileAt t = tile_at<TM, 128, 8>(a);
-    if (t.none) return;
-    const int64_t m0 = (int64_t)t.rt * TM;
-    const int n0 = t.ct * 128 + 32 * wave, rows = (int)min<int64_t>(TM, a.M - m0);
-    const uint32_t ld = (uint32_t)a.KB * BLK * XS;
-    const uint32_t *we_at = a.ws.we + (int64_t)t.ct * ((a.KB + 3) / 4);
-    const WeightRows w_rows(a, n0, l31, h);
-    const Operand x_op = operand(F32 ? reinterpret_cast<const char *>(a.ws.wide) + m0 * ld : reinterpret_cast<const char *>(a.ws.codes) + m0 * ld, (uint32_t)rows * ld);
-    uint32_t off[XC];
-#pragma unroll
-    for (int i = 0; i < XC; ++i) {
-        const int c = wave * XC + i, sub = c / (4 * MBL), row = 8 * (c % (4 * MBL)) + (lane >> 3);
-        off[i] = (uint32_t)min(row, rows - 1) * ld + sub * BLK + (uint32_t)((lane & 7) ^ (row & 7) ^ ((row >> 3) & 1)) * 16;
-    }
-    auto copy_x = [&](int kt, int slot) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < XC; ++i) copy_1k_to_lds(x_op, off[i], (uint32_t)min(kt, a.KB - 1) * (BLK * XS), smem + slot * SLAB + (wave * XC + i) * 1024);
-    };
-    f32x16 acc[1][MBL];
-#pragma unroll
-    for (int j = 0; j < MBL; ++j)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[0][j][r] = 0.f;
-    const uint32_t perm = (uint32_t)((lane & 7) ^ ((lane >> 3) & 1)), row_off = (uint32_t)l31 * BLK;
-    const uint32_t *xe_at = a.ws.xe + m0;
-    int at[MBL];
-    uint32_t xw[MBL];               // words of the step's scales, asked for a step ahead
-#pragma unroll
-    for (int j = 0; j < MBL; ++j) {
-        at[j] = min(32 * j + l31, rows - 1);
-        xw[j] = F32 ? 0 : xe_at[at[j]];
-    }
-    // step kt: W of it in c, x in `slot`; those of step kt + 2 go to `fill` and the slot behind next
-    auto step = [&](int kt, const u32x4 (&c)[4], u32x4 (&fill)[4], int slot) __attribute__((always_inline)) {
-        const int sh = 8 * (kt & 3);
-        const uint32_t ww = uniform_word(we_at + kt / 4);
-        step_barrier<LOADS>();          // x of step kt is there: what is on its way was asked for behind it
-        w_rows.load(kt + 2, fill);
-        copy_x(kt + 2, slot == 0 ? 2 : slot - 1);
-        int xe[MBL];
-#pragma unroll
-        for (int j = 0; j < MBL; ++j) {
-            xe[j] = (int)((xw[j] >> sh) & 0xFF);
-            if (!F32) xw[j] = xe_at[(int64_t)(min(kt + 1, a.KB - 1) / 4) * a.M + at[j]];
-        }
-        const char *xs = smem + slot * SLAB + row_off;
-        const int we = (int)((ww >> sh) & 0xFF);
-        if constexpr (F32) {
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                bf16x8 x[MBL];
-#pragma unroll
-                for (int j = 0; j < MBL; ++j)
-                    x[j] = *reinterpret_cast<const bf16x8 *>(xs + (q >> 2) * SUB + j * 4096 + ((uint32_t)wide_chunk(q & 3, h) ^ perm) * 16);
-                products16(c[q >> 1][2 * (q & 1)], c[q >> 1][2 * (q & 1) + 1], scale_of(we), x, acc);
-            }
-        } else {
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                i32x8 x[MBL];
-                const i32x8 w[1] = {join(c[2 * s], c[2 * s + 1])};
-#pragma unroll
-                for (int j = 0; j < MBL; ++j)
-                    x[j] = join(*reinterpret_cast<const u32x4 *>(xs + j * 4096 + ((uint32_t)(4 * s + h) ^ perm) * 16),
-                                *reinterpret_cast<const u32x4 *>(xs + j * 4096 + ((uint32_t)(4 * s + 2 + h) ^ perm) * 16));
-                products(w, x, we, xe, acc);
-            }
-        }
-    };
-    u32x4 c0[4], c1[4], c2[4];
-    w_rows.load(0, c0);
-    copy_x(0, 0);
-    asm volatile("" ::: "memory");
-    w_rows.load(1, c1);
-    copy_x(1, 1);
-    for (int kt = 0; kt < a.KB; kt += 3) {
-        step(kt, c0, c2, 0);
-        if (kt + 1 >= a.KB) break;
-        step(kt + 1, c1, c0, 1);
-        if (kt + 2 >= a.KB) break;
-        step(kt + 2, c2, c1, 2);
-    }
-    step_barrier<0>();          // (no copy may arrive in LDS that is somebody else's)
-    if (n0 < a.N)
-#pragma unroll
-        for (int j = 0; j < MBL; ++j) store_block<F32>(a, acc[0][j], m0 + 32 * j + l31, n0, h);
-}
-
-template <class K, class... ARGS>
-hipError_t launch_lds(K kern, int64_t blocks, int threads, size_t lds, hipStream_t s, const ARGS &...args)
+template <class K>
+hipError_t launch_lds(K kern, int64_t blocks, size_t lds, const Fp8Args &a, hipStream_t s)
 {
     static const void *configured = nullptr;          // (per kernel type; raised once per kernel)
     if (lds > 65536 && configured != reinterpret_cast<const void *>(kern)) {
@@ -873,57 +620,54 @@ hipError_t launch_lds(K kern, int64_t blocks, int threads, size_t lds, hipStream
         if (e != hipSuccess) return e;
         configured = reinterpret_cast<const void *>(kern);
     }
-    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(threads), lds, s, args...);
+    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(256), lds, s, a);
     return hipGetLastError();
 }
 int64_t tiles_of(const Fp8Args &a, int tm, int tn) { return ((a.M + tm - 1) / tm * ((a.N + tn - 1) / tn) + 7) / 8 * 8; }
-template <int MBL, bool F32, bool RAW, int RING>
-hipError_t launch_few(const Fp8Args &a, const FewX &fx, hipStream_t s)
-{
-    return launch_lds(project_fp8_few_kernel<MBL, F32, RAW, RING>, (a.N + 31) / 32, FW * 64, (size_t)FW / 2 * MBL * 4096, s, a, fx);
-}
-template <int MBL, bool F32>
-hipError_t launch_stream(const Fp8Args &a, hipStream_t s)
-{
-    return launch_lds(project_fp8_stream_kernel<MBL, F32>, tiles_of(a, 32 * MBL, 128), 256, (size_t)3 * MBL * (F32 ? 8192 : 4096), s, a);
-}
 template <class T>
 hipError_t launch_tile(const Fp8Args &a, hipStream_t s)
 {
-    return launch_lds(project_fp8_tile_kernel<T>, tiles_of(a, T::TM, T::TN), 256, T::LDS, s, a);
+    return launch_lds(project_fp8_tile_kernel<T>, tiles_of(a, T::TM, T::TN), T::LDS, a, s);
 }
-typedef MidTile<128, 128, 4, 1> Tile128;
-typedef MidTile<192, 128, 4, 1> Tile192;
-typedef MidTile<256, 128, 3, 1> Tile256;
+// Tiles, with as many of their steps as LDS holds.
+typedef Tile<64, 64, 8, false> T64;
+typedef Tile<64, 128, 6, false, true> T64W;
+typedef Tile<128, 128, 4, false> T128;
+typedef Tile<192, 128, 4, false> T192;
+typedef Tile<256, 128, 3, false> T256;
+typedef Tile<64, 64, 6, true> F64;
+typedef Tile<64, 128, 4, true, true> F64W;
+typedef Tile<128, 128, 3, true> F128;
 
-enum ProductKind { FEW_RAW = 1, FEW, STREAM, TILE_128, TILE_192, TILE_256, BIG };
-#ifdef SGC_TUNE
-extern "C" int sgc_tune_kind = 0;
-#endif
-ProductKind product_kind(int64_t M, int N, int x_dtype, int y_dtype)
-{
-#ifdef SGC_TUNE
-    if (sgc_tune_kind) return (ProductKind)sgc_tune_kind;
-#endif
-    
-    if (M <= 64 && N < 12288) return FEW;
-    if (y_dtype == SGC_F32 || M <= 64) return STREAM;
-    Fp8Args a{};
-    a.M = M;
-    a.N = N;
-    return tiles_of(a, 256, 256) >= 192 ? BIG : TILE_128;
-}
+// Which tile a product is computed in: the one whose rounds over the 256 compute units cost least, at so much a step (us per 128 codes,
+// fitted to one and two rounds of 4096 codes).  us, chosen / next best: 20 x 6144 64x64 10.8 / 13.7 (64x128); 64 x 28672 64x128 27.7 / 32.7 (64x64);
+// 64 x 50021 64x128 50.5 / 58.8; 128 x 50021 128x128 62 / 78 (64x128); 640 x 4096 128x128 22 / 27 (192x128); 1280 x 4096 192x128 31 / 35 (256x128);
+// 1280 x 6144 256x128 39 / 42 (128x128); 2048 x 6144 256x256 54 / 62 (128x128).  fp32: 64 x 6144 64x64 18.4 / 19.9; 64 x 50021 64x128 54.6 / 63.2 (128x128);
+// 1280 x 50021 128x128 536 / 630 (64x128).
+struct Choice {
+    int tm, tn;
+    float step;
+    hipError_t (*launch)(const Fp8Args &, hipStream_t);
+};
+hipError_t launch_big(const Fp8Args &a, hipStream_t s) { return launch_lds(project_fp8_big_kernel, tiles_of(a, 256, 256), BIG_LDS, a, s); }
+constexpr Choice kTiles[] = {{64, 64, 0.25f, launch_tile<T64>},    {64, 128, 0.40f, launch_tile<T64W>},  {128, 128, 0.53f, launch_tile<T128>},
+                             {192, 128, 0.78f, launch_tile<T192>}, {256, 128, 0.98f, launch_tile<T256>}, {256, 256, 1.45f, launch_big}};
+constexpr Choice kTilesF32[] = {{64, 64, 0.42f, launch_tile<F64>}, {64, 128, 0.50f, launch_tile<F64W>}, {128, 128, 0.72f, launch_tile<F128>}};
 
-template <bool F32>
-hipError_t launch_products(const Fp8Args &a, const FewX &fx, ProductKind kind, hipStream_t s)
+template <size_t N>
+hipError_t launch_best(const Choice (&choices)[N], const Fp8Args &a, hipStream_t s)
 {
-    if (kind == FEW_RAW) return launch_few<1, F32, true, 3>(a, fx, s);
-    if (kind == FEW) return a.M <= 32 ? launch_few<1, F32, false, 3>(a, fx, s) : launch_few<2, F32, false, 2>(a, fx, s);
-    if (kind == STREAM || F32) return a.M <= 32 ? launch_stream<1, F32>(a, s) : a.M <= 64 ? launch_stream<2, F32>(a, s) : launch_stream<4, F32>(a, s);
-    if (kind == TILE_128) return launch_tile<Tile128>(a, s);
-    if (kind == TILE_192) return launch_tile<Tile192>(a, s);
-    if (kind == TILE_256) return launch_tile<Tile256>(a, s);
-    return launch_lds(project_fp8_big_kernel, tiles_of(a, 256, 256), 256, BIG_LDS, s, a);
+    const Choice *best = nullptr;
+    float least = 0.f;
+    for (const Choice &c : choices) {
+        const int64_t tiles = ((a.M + c.tm - 1) / c.tm) * ((a.N + c.tn - 1) / c.tn);
+        const float cost = (float)((tiles + 255) / 256) * c.step;
+        if (!best || cost < least) {
+            best = &c;
+            least = cost;
+        }
+    }
+    return best->launch(a, s);
 }
 
 size_t round16(size_t x) { return (x + 15) / 16 * 16; }
@@ -995,20 +739,15 @@ int sgc_project_fp8(sgc_ctx *ctx, const void *dev_x, int32_t x_dtype, int64_t x_
     a.M = n_rows;
     a.N = n_features;
     a.KB = KB;
-    const ProductKind kind = product_kind(n_rows, n_features, x_dtype, y_dtype);
+    const int64_t x_groups = (n_rows * KB4 + 3) / 4, w_groups = ((int64_t)NB * KB4 + 255) / 256;
     const uint8_t *exps = static_cast<const uint8_t *>(dev_exponents);
-    const FewX fx{static_cast<const uint16_t *>(dev_x), x_stride, d_model, exps};
-    hipError_t e = hipSuccess;
-    if (kind != FEW_RAW) {
-        const int64_t x_groups = (n_rows * KB4 + 3) / 4, w_groups = ((int64_t)NB * KB4 + 255) / 256;
-        const dim3 qgrid((unsigned)(x_groups + w_groups));
-        if (x_dtype == SGC_F32)
-            hipLaunchKernelGGL(quantise_rows_kernel<float>, qgrid, dim3(256), 0, s, static_cast<const float *>(dev_x), x_stride, n_rows, d_model, a.ws, exps, NB, (int)x_groups);
-        else
-            hipLaunchKernelGGL(quantise_rows_kernel<uint16_t>, qgrid, dim3(256), 0, s, static_cast<const uint16_t *>(dev_x), x_stride, n_rows, d_model, a.ws, exps, NB, (int)x_groups);
-        e = hipGetLastError();
-    }
-    if (e == hipSuccess) e = y_dtype == SGC_F32 ? launch_products<true>(a, fx, kind, s) : launch_products<false>(a, fx, kind, s);
+    const dim3 qgrid((unsigned)(x_groups + w_groups));
+    if (x_dtype == SGC_F32)
+        hipLaunchKernelGGL(quantise_rows_kernel<float>, qgrid, dim3(256), 0, s, static_cast<const float *>(dev_x), x_stride, n_rows, d_model, a.ws, exps, NB, (int)x_groups);
+    else
+        hipLaunchKernelGGL(quantise_rows_kernel<uint16_t>, qgrid, dim3(256), 0, s, static_cast<const uint16_t *>(dev_x), x_stride, n_rows, d_model, a.ws, exps, NB, (int)x_groups);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess) e = y_dtype == SGC_F32 ? launch_best(kTilesF32, a, s) : launch_best(kTiles, a, s);
     if (e != hipSuccess) return report(ctx, SGC_EHIP, "project_fp8 kernels: %s", hipGetErrorString(e));
     return SGC_OK;
 }
