@@ -28,6 +28,7 @@
 #include <type_traits>
 
 #include "sgc_internal.h"
+#include "sgc_draft_rows.h"
 #include "sgc_own_keys.h"
 
 namespace sgc {
@@ -79,18 +80,6 @@ __device__ inline uint32_t fp8x2_to_16x2(uint32_t w, bool high)
     }
     const auto r = high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false);
     return __builtin_bit_cast(uint32_t, r);
-}
-
-// A record that no launch writes while it is read, at a wave-uniform address: through the scalar path, into scalar registers.
-// (The compiler must take a plain load for one that a store of the same kernel could change, and fetch it per lane.)
-template <typename T>
-__device__ inline T uniform_record(const T *p)
-{
-    const auto *words = (const __attribute__((address_space(4))) uint32_t *)p;
-    uint32_t w[sizeof(T) / 4];
-#pragma unroll
-    for (size_t i = 0; i < sizeof(T) / 4; ++i) w[i] = words[i];
-    return __builtin_bit_cast(T, w);
 }
 
 // V operands of two pages of token rows: eight blocks (page i / 4, 32-channel group i % 4) for the second product, read
@@ -221,7 +210,10 @@ __device__ __forceinline__ const AttnArgs &attn_args(const ARGS &c) { return c.a
 // way into LDS; otherwise they are read from the suffix page pool.
 //
 // ARGS: AttnArgs, or CarriedSuffix / CarriedPrefix, whose tables are read where they arrive, among the launch's arguments.
-template <bool KV_FP8, int MODE, bool QK8, bool OWN_RAW, typename ARGS>
+//
+// DRAFT: a pass over drafted tokens.  A tile's rows are numbered through the tokens that the cluster's queries bring to this pass, whose
+// counts are on the device; tiles behind the last of them end at once.  The cached keys alone, key ranges in fp32.
+template <bool KV_FP8, int MODE, bool QK8, bool OWN_RAW, typename ARGS, bool DRAFT = false>
 __global__ void __launch_bounds__(NW * 64, 2) attn_mfma_kernel(const ARGS args)
 {
     constexpr bool CARRIED = !std::is_same_v<ARGS, AttnArgs>;
@@ -229,7 +221,8 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_mfma_kernel(const ARGS args)
     const AttnArgs &a = attn_args(args);
     static_assert(NW == 4 && MI == 1, "the own-suffix part deals pages to four wavefronts of 32 rows");
     static_assert(!QK8 || KV_FP8, "the fp8 first product needs an fp8 cache");
-    if (!CARRIED && MODE == MODE_SUFFIX && (int)blockIdx.x >= a.n_tiles) {
+    static_assert(!DRAFT || (!CARRIED && MODE == MODE_SUFFIX && !OWN_RAW), "drafted tokens: tables on the device, own keys elsewhere");
+    if (!CARRIED && !DRAFT && MODE == MODE_SUFFIX && (int)blockIdx.x >= a.n_tiles) {
         append_new_tokens(a, (int)blockIdx.x - a.n_tiles);
         return;
     }
@@ -308,6 +301,13 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_mfma_kernel(const ARGS args)
             lse_stride = t.prefix_len;
             t.tok_base = 0;
         }
+    }
+    DraftRow draft = {0, 0, 0, 0, 0, 0};
+    if constexpr (DRAFT) {
+        int tokens;
+        draft = draft_row<false>(a, __builtin_amdgcn_readfirstlane(t.sq_lo), __builtin_amdgcn_readfirstlane(t.sq_hi), (t.row0 + wave * 32 + n) / g, tokens);
+        t.n_rows = min(t.n_rows, tokens * g - t.row0);
+        if (t.n_rows <= 0) return;
     }
     // decode tiles cover one key range of the cluster's cache: own output set, positions continue behind ALL cached keys
     const int key_range = __builtin_amdgcn_readfirstlane(t.pad) >> 24;
@@ -449,7 +449,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_mfma_kernel(const ARGS args)
     }
     // Own keys are numbered by slots, 16 to a page, over the own pages of all queries the tile touches: page 0 is the
     // first page of the tile's first query, and the last one holds the tile's last row's own key.
-    const bool own = MODE == MODE_SUFFIX && !a.skip_self;
+    const bool own = !DRAFT && MODE == MODE_SUFFIX && !a.skip_self;
     const int own_page0 = __builtin_amdgcn_readfirstlane(t.own_page0), n_own = own ? __builtin_amdgcn_readfirstlane(t.n_own_pages) : 0;
     bool valid[MI];
     int64_t io_row[MI];     // element offset of the row in q / o
@@ -462,7 +462,11 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_mfma_kernel(const ARGS args)
         const int rc = valid[mi] ? r : last_row;
         const int tk = rc / g;
         head[mi] = hk * g + (rc - tk * g);
-        if (MODE == MODE_SUFFIX) {
+        if constexpr (DRAFT) {
+            src_tok[mi] = draft.src;
+            qpos[mi] = draft.qpos;
+            lim[mi] = P;
+        } else if (MODE == MODE_SUFFIX) {
             const int tau = tok_base + tk;
             if (inline_queries) {        // which of the (at most 4) queries of the tile record the token belongs to
                 const bool ge1 = tau >= tq_tok0[1], ge2 = tau >= tq_tok0[2], ge3 = tau >= tq_tok0[3];
@@ -475,7 +479,6 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_mfma_kernel(const ARGS args)
                 const TokInfo ti = a.tok_info[tau];
                 src_tok[mi] = ti.src;
                 qpos[mi] = ti.qpos;
-                if (a.done) qpos[mi] += min(min(max(a.done[ti.draft >> 5], 0), a.done_cap) + (ti.draft & 31), a.done_cap - 1);
                 own_first = (ti.own0 - own_page0) * kPageTokens;
             }
             lim[mi] = P;
@@ -803,6 +806,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_mfma_kernel(const ARGS args)
     // and V of tile kt are read.  At the top of step kt a wavefront holds the scores of (kt, half 0) and, in
     // its window, the K blocks of (kt, half 1).
     const int n_my = min(n_kt, (lim_max + BN - 1) / BN);      // tiles this wavefront has rows for
+    const bool mine = !DRAFT || wave_u * 32 < t.n_rows;       // the wavefront has rows at all (one without leaves the matrix cores to the others)
     f32x16 s0[MI], s1[MI];
     if (n_kt > 0) {
         if (KV_FP8) {      // through registers: one tile's worth at a time
@@ -957,7 +961,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_mfma_kernel(const ARGS args)
         }
         pg_v = pg_k;
         pg_k = pg_new;
-        if (spread || MODE == MODE_SUFFIX || kt < n_my) {  // some row of this wave still sees keys of this tile
+        if (DRAFT ? spread || mine : spread || MODE == MODE_SUFFIX || kt < n_my) {  // some row of this wave still sees keys of this tile
             const int key0 = kt * BN;
             const bool masked = key0 + BN > lim_min;
             const bool careful = masked || fresh;
@@ -1008,7 +1012,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_mfma_kernel(const ARGS args)
     {
         int kt = 0;
         if (!KV_FP8) {
-            const int n_spread = min(n_kt - 2, MODE == MODE_SUFFIX ? n_kt : n_my);
+            const int n_spread = DRAFT && !mine ? 0 : min(n_kt - 2, MODE == MODE_SUFFIX ? n_kt : n_my);
             for (; kt < n_spread; ++kt) cache_step(kt, std::integral_constant<int, SPREAD>{});
         }
         for (; kt < n_kt - 1; ++kt) cache_step(kt, std::integral_constant<int, TOP>{});
@@ -1092,7 +1096,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_mfma_kernel(const ARGS args)
     // 8 KiB of the K and V buffers that the chunk after the last own one would take (every wavefront is past the barrier behind
     // their last read), the 16-byte chunks of row n permuted by n % 16 so that the writes and the reads below spread over all banks, and stores
     // four whole rows of 256 bytes per instruction.
-    if (!CARRIED && MODE == MODE_SUFFIX && a.done) {
+    if constexpr (DRAFT) {
         // A pass over drafted tokens adds its key ranges up in fp32 (rounded to bf16 here the outputs were off by 2.8e-3 instead of 2.1e-3,
         // 2-norm): a lane stores its pieces of four channels as they are.
         float *of = static_cast<float *>(o_base);
@@ -1147,11 +1151,11 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_mfma_kernel(const ARGS args)
     }
 }
 
-template <bool FP8, int MODE, bool QK8, bool OWN_RAW, typename ARGS>
+template <bool FP8, int MODE, bool QK8, bool OWN_RAW, typename ARGS, bool DRAFT = false>
 hipError_t launch_one(const ARGS &a, int blocks, hipStream_t s)
 {
     static bool configured = false;     // raise the dynamic LDS limit once per instantiation
-    auto kern = attn_mfma_kernel<FP8, MODE, QK8, OWN_RAW, ARGS>;
+    auto kern = attn_mfma_kernel<FP8, MODE, QK8, OWN_RAW, ARGS, DRAFT>;
     const size_t lds = 4 * HALF_BYTES;      // two K buffers, two V buffers
     if (!configured) {
         hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -1175,29 +1179,6 @@ hipError_t launch_one(const ARGS &a, int blocks, hipStream_t s)
 // cluster served by itself would no longer equal the same cluster in a batch bit for bit.  A step's ranges follow from the call
 // as it is.)
 constexpr int NWF = 8;        // wavefronts of a workgroup
-
-// Memory that workgroups of one launch hand to each other: stored through to and loaded from the level that all XCDs share (agent-scope
-// accesses).  A release and an acquire fence instead write back and invalidate a whole XCD's L2, under the other workgroups' reads
-// of the cache: 16 prompts of 1000 tokens in two ranges 27 us a step.
-template <typename T>
-__device__ __forceinline__ void store_shared(T *p, const T &v)
-{
-    static_assert(sizeof(T) % 8 == 0, "eight bytes at a time");
-    uint64_t w[sizeof(T) / 8];
-    __builtin_memcpy(w, &v, sizeof(T));
-#pragma unroll
-    for (size_t i = 0; i < sizeof(T) / 8; ++i) __hip_atomic_store(reinterpret_cast<uint64_t *>(p) + i, w[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-template <typename T>
-__device__ __forceinline__ T load_shared(const T *p)
-{
-    uint64_t w[sizeof(T) / 8];
-#pragma unroll
-    for (size_t i = 0; i < sizeof(T) / 8; ++i) w[i] = __hip_atomic_load(reinterpret_cast<const uint64_t *>(p) + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    T v;
-    __builtin_memcpy(&v, w, sizeof(T));
-    return v;
-}
 
 __global__ void __launch_bounds__(NWF * 64, 2) attn_few_kernel(const AttnArgs a)
 {
@@ -1558,6 +1539,10 @@ hipError_t launch_attn_mfma(const AttnArgs &a, hipStream_t s)
     const bool fp8 = a.pool.kv_dtype == SGC_FP8_E4M3;
     if (a.n_tiles <= 0 && a.n_append <= 0) return hipSuccess;
     if (a.few) return launch_few(a, s);
+    if (a.done) {
+        if (fp8 && a.fp8_first_product) return launch_one<true, MODE_SUFFIX, true, false, AttnArgs, true>(a, a.n_tiles, s);
+        return fp8 ? launch_one<true, MODE_SUFFIX, false, false, AttnArgs, true>(a, a.n_tiles, s) : launch_one<false, MODE_SUFFIX, false, false, AttnArgs, true>(a, a.n_tiles, s);
+    }
     if (a.mode == MODE_SUFFIX) {
         // a decode step's launch carries, behind its tiles, the blocks that append the step's new tokens
         const int per_block = NW * 64 / 8;

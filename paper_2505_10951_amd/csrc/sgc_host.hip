@@ -680,9 +680,11 @@ void build_decode_tiles(sgc_plan *pl, int tile_rows)
     for (size_t sq = 0; sq < pl->sq_len.size(); ++sq) pl->dtok[sq] = {pl->sq_query[sq], pl->sq_len[sq], pl->sq_page0[sq], 0};
 }
 
-// Row tiles of passes over drafted tokens: max_rows x g rows per query, all queries of a (cluster, KV head) stacked, the cached keys of
-// every row tile split into ranges as for decode steps.  A pass has max_rows times a step's rows, and more tiles of its own to fill the
-// chip with.
+// Row tiles of passes over drafted tokens: max_rows x g rows per query at most, all queries of a (cluster, KV head) stacked, the keys of
+// every row tile split into S ranges.
+// One launch (draft_few_kernel) where a cluster and KV head have few rows; its tiles are 32 rows, over cached and own keys alike.
+// Two otherwise: 128 rows over the cached keys, whose ranges are dealt as for decode steps, and long ones cut into at most 48 steps of 64 keys, so that
+// tiles that end up without rows leave no compute unit idle (64 queries of up to 8 tokens, 64 heads, prompts of 16384: S = 2, 4, 6, 8 239, 219, 217, 211 us).
 void build_draft_tiles(sgc_plan *pl, int tile_rows)
 {
     const sgc_ctx *ctx = pl->ctx;
@@ -694,47 +696,63 @@ void build_draft_tiles(sgc_plan *pl, int tile_rows)
     };
     std::vector<Unit> units;
     std::vector<double> work;
-    int64_t row_tiles = 0, max_steps = 0;
+    int64_t max_steps = 0, row_tiles = 0, few_tiles = 0, own = 0;
     for (int c = 0; c < pl->n_clusters; ++c) {
         const int64_t rows = (pl->cl_sq_off[c + 1] - pl->cl_sq_off[c]) * per_query;
         if (rows == 0) continue;
-        const int64_t nt = (rows + tile_rows - 1) / tile_rows;
-        row_tiles += nt * ctx->p.n_kv_heads;
+        // units of own and new tokens that a tile of 32 rows meets
+        int64_t most_own = 0;
+        for (int32_t sq = pl->cl_sq_off[c]; sq < pl->cl_sq_off[c + 1]; ++sq) most_own = std::max<int64_t>(most_own, (pl->sq_len[sq] + pl->decode_cap + 31) / 32 + 1);
+        own = std::max(own, std::min<int64_t>(pl->cl_sq_off[c + 1] - pl->cl_sq_off[c], 31 / per_query + 1) * most_own);
+        row_tiles += (rows + tile_rows - 1) / tile_rows * ctx->p.n_kv_heads;
+        few_tiles += (rows + 31) / 32 * ctx->p.n_kv_heads;
         max_steps = std::max<int64_t>(max_steps, (pl->cl_prefix_len[c] + 63) / 64);
         for (int hk = 0; hk < ctx->p.n_kv_heads; ++hk) {
             units.push_back({c, hk, rows});
-            work.push_back((double)nt * (pl->cl_prefix_len[c] + 64.0));
+            work.push_back((double)rows * (pl->cl_prefix_len[c] + 64.0));
         }
     }
+    // One launch while its tiles' work, in rounds over 256 compute units of a fixed part (that of 20 units of 32 keys) and their units
+    // (an own or new one counts as two cached ones: it is masked, and new keys are rotated), stays under 84 such units.  80 drawn
+    // shapes: under it 0.55 to 0.97 times the two launches' time but for two (1.03, 1.10), above it 1.05 to 2.7 times but for two.
+    // 1 query of 5 tokens, 32 heads on 8, prompt of 411: 13.4 against 20.8 us; 10 prompts of 1024, 320 queries: 108 against 69 us.
+    const int few_splits = (int)std::max<int64_t>(1, std::min<int64_t>({(2 * max_steps + 17) / 16, 256 / std::max<int64_t>(few_tiles, 1), kDecodeMaxSplits}));
+    pl->draft_few = (few_tiles * few_splits + 255) / 256 * (20 + (2 * max_steps + 2 * own) / few_splits) <= 84;
+    if (pl->draft_few) tile_rows = 32;
     int S = 1;
-    if (row_tiles > 0) {
+    if (pl->draft_few) S = few_splits;
+    else if (row_tiles > 0) {
         const int64_t full = std::min(max_steps / 8, std::max<int64_t>(512 / row_tiles, 1)), half = std::min({max_steps / 3, std::max<int64_t>(256 / row_tiles, 1), (int64_t)8});
-        S = (int)std::min<int64_t>(kDecodeMaxSplits, std::max({(int64_t)1, full, half}));
+        S = (int)std::min<int64_t>(kDecodeMaxSplits, std::max({(int64_t)1, full, half, std::min<int64_t>((max_steps + 47) / 48, 8)}));
     }
     if (max_steps >= (1 << 24) / 64) S = 1;      // the position offset travels in 24 bits of the tile record
     pl->draft_splits = S;
     std::array<std::vector<std::pair<Tile, int32_t>>, kXcd> lists;
     const auto of_xcd = deal_to_xcds(work);
+    int32_t n_row_tiles = 0;
     for (int x = 0; x < kXcd; ++x)
         for (int ui : of_xcd[x]) {
             const Unit &u = units[ui];
             const int P = pl->cl_prefix_len[u.cluster], steps = (P + 63) / 64;
-            for (int64_t r = 0; r < u.rows; r += tile_rows)
+            for (int64_t r = 0; r < u.rows; r += tile_rows, ++n_row_tiles)
                 for (int sp = 0; sp < S; ++sp) {
-                    const int key0 = std::min(P, 64 * (int)((int64_t)steps * sp / S)), key1 = std::min(P, 64 * (int)((int64_t)steps * (sp + 1) / S));
+                    // (one launch: from the range's first unit of 32 keys to the prompt's end; where it ends the kernel finds itself)
+                    const int key0 = pl->draft_few ? 32 * (int)((int64_t)((P + 31) / 32) * sp / S) : std::min(P, 64 * (int)((int64_t)steps * sp / S));
+                    const int key1 = pl->draft_few ? P : std::min(P, 64 * (int)((int64_t)steps * (sp + 1) / S));
                     Tile t{};
                     t.cluster = u.cluster;
                     t.hk = u.hk;
                     t.row0 = (int32_t)r;
                     t.n_rows = (int32_t)std::min<int64_t>(tile_rows, u.rows - r);
                     t.prefix_len = key1 - key0;
-                    t.pad = (sp << 24) | (P - t.prefix_len);
-                    t.tok_base = pl->cl_sq_off[u.cluster] * R;
-                    t.sq_hi = -1;
-                    t.n_q = kTileQueries + 1;             // row bookkeeping from the table
+                    t.pad = (sp << 24) | (pl->draft_few ? key0 : P - t.prefix_len);
+                    t.sq_lo = pl->cl_sq_off[u.cluster];          // the cluster's queries: rows are numbered through what they bring
+                    t.sq_hi = pl->cl_sq_off[u.cluster + 1] - 1;
+                    t.row_tile = n_row_tiles;
                     lists[x].push_back({t, key0});
                 }
         }
+    pl->draft_row_tiles = n_row_tiles;
     size_t slots = 0;
     for (auto &l : lists) slots = std::max(slots, l.size());
     pl->ftiles.assign(slots * kXcd, Tile{});
@@ -744,9 +762,6 @@ void build_draft_tiles(sgc_plan *pl, int tile_rows)
             pl->ftiles[k * kXcd + x] = lists[x][k].first;
             pl->ftile_key0[k * kXcd + x] = lists[x][k].second;
         }
-    pl->ftok.resize(pl->sq_len.size() * R);
-    for (size_t sq = 0; sq < pl->sq_len.size(); ++sq)
-        for (int j = 0; j < R; ++j) pl->ftok[sq * R + j] = {pl->sq_query[sq] * R + j, pl->sq_len[sq], pl->sq_page0[sq], pl->sq_query[sq] << 5 | j};
 }
 
 void plan_free_device(sgc_plan *pl)
@@ -1376,6 +1391,9 @@ static ExpandArgs plan_expand_args(const sgc_plan *pl, const sgc_cache *c)
 // with_tiles: the cache's device tables are current and ordered in front of what comes next on the stream, as a suffix prefill
 // has them; the tile records are then written behind the copy.
 // cache (may be null): its page tables, if due, go with the same launch.
+static size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+// A pass in one launch: the ranges' partial results, behind which the row tiles' counters lie.
+static size_t draft_few_bytes(const sgc_plan *pl) { return pl->draft_splits > 1 ? round256((size_t)pl->draft_row_tiles * pl->draft_splits * kFewPartBytes) : 0; }
 // Partial results of a key range of a pass over drafted tokens: outputs [n_queries][rows][Hq][d] fp32, then log-sum-exps [Hq][n_queries rows].
 struct DraftParts {
     size_t o, set;
@@ -1383,8 +1401,8 @@ struct DraftParts {
 static DraftParts draft_part_bytes(const sgc_plan *pl)
 {
     const size_t rows = (size_t)pl->n_queries * pl->draft_rows * pl->ctx->p.n_q_heads;
-    const size_t o = (rows * pl->ctx->p.head_dim * sizeof(float) + 255) / 256 * 256;
-    return {o, o + (rows * sizeof(float) + 255) / 256 * 256};
+    const size_t o = round256(rows * pl->ctx->p.head_dim * sizeof(float));
+    return {o, o + round256(rows * sizeof(float))};
 }
 
 static int plan_upload(sgc_plan *pl, hipStream_t s, bool with_tiles, sgc_cache *cache)
@@ -1396,7 +1414,6 @@ static int plan_upload(sgc_plan *pl, hipStream_t s, bool with_tiles, sgc_cache *
     pl->dtiles.clear();
     pl->dtok.clear();
     pl->ftiles.clear();
-    pl->ftok.clear();
     if (want_rows > 0) {
         if (pl->tile_rows != want_rows) build_tiles(pl, want_rows);      // (a small call may have built them)
         if (pl->decode_cap > 0) build_decode_tiles(pl, want_rows);
@@ -1445,7 +1462,6 @@ static int plan_upload(sgc_plan *pl, hipStream_t s, bool with_tiles, sgc_cache *
         {pl->dtiles.data(), pl->dtiles.size() * sizeof(Tile), (const void **)&pl->d_dtiles},
         {pl->dtok.data(), pl->dtok.size() * sizeof(TokInfo), (const void **)&pl->d_dtok},
         {pl->ftiles.data(), pl->ftiles.size() * sizeof(Tile), (const void **)&pl->d_ftiles},
-        {pl->ftok.data(), pl->ftok.size() * sizeof(TokInfo), (const void **)&pl->d_ftok},
         // the tile records are written on the device, from the seeds
         {nullptr, pl->tiles.size() * sizeof(Tile), (const void **)&pl->d_tiles},
     };
@@ -1486,7 +1502,11 @@ static int plan_upload(sgc_plan *pl, hipStream_t s, bool with_tiles, sgc_cache *
         pl->d_spool = pl->spool_block.p;
         if (pl->decode_cap > 0) SGC_HIP(ctx, launch_fill_zero_bytes(pl->d_spool, pl->spool_bytes, s));
     }
-    if (pl->draft_rows > 0 && (rc = dev_acquire(ctx, draft_part_bytes(pl).set * pl->draft_splits, s, &pl->draft_scratch)) != SGC_OK) return rc;
+    if (pl->draft_rows > 0) {
+        const size_t bytes = pl->draft_few ? draft_few_bytes(pl) + round256(pl->draft_row_tiles * sizeof(uint32_t)) : draft_part_bytes(pl).set * pl->draft_splits;
+        if ((rc = dev_acquire(ctx, bytes, s, &pl->draft_scratch)) != SGC_OK) return rc;
+        if (pl->draft_few) SGC_HIP(ctx, launch_fill_zero_bytes(pl->draft_scratch.p + draft_few_bytes(pl), round256(pl->draft_row_tiles * sizeof(uint32_t)), s));
+    }
     pl->uploaded = true;
     return SGC_OK;
 }
@@ -2061,11 +2081,25 @@ int sgc_draft_step_batched(sgc_ctx *ctx, const sgc_cache *cc, sgc_plan *pl, int3
     a.mode = MODE_SUFFIX;
     a.tiles = pl->d_ftiles;
     a.n_tiles = (int32_t)pl->ftiles.size();
-    a.tok_info = pl->d_ftok;
     a.spool = spool;
-    a.skip_self = 1;
+    a.sq_query = pl->d_sq_query;
+    a.sq_len = pl->d_sq_len;
     a.done = dev_done;
+    a.rows = dev_rows;
+    a.max_rows = pl->draft_rows;
     a.done_cap = pl->decode_cap;
+    if (pl->draft_few) {
+        a.k = dev_k;
+        a.v = dev_v;
+        a.o = dev_o;
+        a.lse = dev_lse;
+        a.sq_page0 = pl->d_sq_page0;
+        a.n_ranges = pl->draft_splits;
+        a.parts = scratch;
+        a.arrived = reinterpret_cast<uint32_t *>(scratch + draft_few_bytes(pl));
+        SGC_HIP(ctx, launch_draft_few(a, s));
+        return SGC_OK;
+    }
     a.o = scratch;
     a.lse = reinterpret_cast<float *>(scratch + part.o);
     a.split_o_bytes = (int64_t)part.set;

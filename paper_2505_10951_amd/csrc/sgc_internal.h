@@ -168,7 +168,7 @@ struct TokInfo {
     int32_t src;    // row of the token in the caller's packed arrays
     int32_t qpos;   // index of the token inside its query
     int32_t own0;   // first own page of the query (records of decode steps: its first page in the suffix page pool)
-    int32_t draft;  // records of passes over drafted tokens: query << 5 | number of the token in the pass
+    int32_t unused;
 };
 
 // One cluster of a (batched) prefix prefill.
@@ -211,6 +211,17 @@ struct DecodeArgs {
     int32_t use_mfma;             // head_dim 128 and 16-bit rows: the matrix-core form of the own-keys kernel may run
     float scale_log2e;
 };
+
+// How many generated tokens of a query are in its pages, and how many rows it brings to a pass over drafted tokens: none where a count is out of
+// range, and none that the pages have no room for.
+struct DraftCount {
+    int32_t done, rows;
+};
+__device__ inline DraftCount draft_count(const int32_t *done, const int32_t *rows, int32_t n, int32_t max_rows, int32_t cap)
+{
+    const int32_t d = done[n], r = rows ? min(rows[n], max_rows) : max_rows;
+    return {d, d < 0 || d >= cap || r < 1 ? 0 : min(r, cap - d)};
+}
 
 // A pass over drafted tokens: arguments of the kernel for the queries' own keys (sgc_draft.hip).
 constexpr int kDraftMaxRows = 16;         // new tokens of a query: one page of keys
@@ -362,10 +373,9 @@ struct AttnArgs {
     int32_t n_ranges;
     // fp8 cache: run the first product on the e4m3 codes, with the query quantised per row (suffix mode)
     int32_t fp8_first_product;
-    // passes over drafted tokens: a row's position lies done[query] + its number in the pass behind its query's question (never at or
-    // behind done_cap: rows that the pass does not have are computed somewhere and not used).  Null otherwise.
-    const int32_t *done;
-    int32_t done_cap;
+    // passes over drafted tokens (done null: none): counts as in DraftArgs
+    const int32_t *done, *rows;
+    int32_t max_rows, done_cap;
 };
 
 // ---- small calls: tables with the launch ----------------------------------------------------------------------------------
@@ -535,11 +545,10 @@ struct sgc_plan {
     int32_t draft_rows = 0;
     std::vector<sgc::Tile> ftiles;
     std::vector<int32_t> ftile_key0;
-    std::vector<sgc::TokInfo> ftok;
-    int32_t draft_splits = 1;
+    int32_t draft_splits = 1, draft_row_tiles = 0;
+    bool draft_few = false;                   // passes are one launch of the kernel for few rows
     sgc_dev_block draft_scratch;
     const sgc::Tile *d_ftiles = nullptr;
-    const sgc::TokInfo *d_ftok = nullptr;
     size_t spool_layer_bytes = 0;
     sgc_dev_block dec_scratch;                // cached-prefix part of a decode step: O then LSE
     uint64_t dec_counters_cleared = 0;        // its counters: see clear_step_counters
@@ -646,6 +655,8 @@ hipError_t launch_attn_generic(const CarriedGeneric &c, int n_gtiles, hipStream_
 hipError_t launch_decode_own_keys(const DecodeArgs &d, hipStream_t s);
 // Passes over drafted tokens, behind the cached part: own keys, new ones among them, the sum, and the new keys' way into the pages.
 hipError_t launch_draft_own_keys(const DraftArgs &d, hipStream_t s);
+// Passes of few rows: all of it in one launch (tiles of 32 rows; parts, arrived and n_ranges as for decode steps of few rows).
+hipError_t launch_draft_few(const AttnArgs &a, hipStream_t s);
 hipError_t launch_fill_zero_bytes(void *p, size_t bytes, hipStream_t s);
 // bytes (a multiple of 4, both pointers 16-byte aligned) from mapped host memory to device memory, read by a kernel;
 // optionally a second piece in the same launch; expand (may be null): tile records to write behind the copy
