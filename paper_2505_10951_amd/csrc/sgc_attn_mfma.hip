@@ -302,13 +302,6 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_mfma_kernel(const ARGS args)
             t.tok_base = 0;
         }
     }
-    DraftRow draft = {0, 0, 0, 0, 0, 0};
-    if constexpr (DRAFT) {
-        int tokens;
-        draft = draft_row<false>(a, __builtin_amdgcn_readfirstlane(t.sq_lo), __builtin_amdgcn_readfirstlane(t.sq_hi), (t.row0 + wave * 32 + n) / g, tokens);
-        t.n_rows = min(t.n_rows, tokens * g - t.row0);
-        if (t.n_rows <= 0) return;
-    }
     // decode tiles cover one key range of the cluster's cache: own output set, positions continue behind ALL cached keys
     const int key_range = __builtin_amdgcn_readfirstlane(t.pad) >> 24;
     const int pos_extra = __builtin_amdgcn_readfirstlane(t.pad) & 0xFFFFFF;
@@ -324,7 +317,6 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_mfma_kernel(const ARGS args)
     const int n_pages = (P + kPageTokens - 1) / kPageTokens;
     const int32_t *pt = page_table + __builtin_amdgcn_readfirstlane(t.pt_off);
     const int tok_base = __builtin_amdgcn_readfirstlane(t.tok_base);
-    const int last_row = t.row0 + t.n_rows - 1;
 
     // ---- copy machinery ----------------------------------------------------------------------------
     // A tile is 8 parts: K of its 4 pages, then V of its 4 pages; a part is 4 KiB of bf16 (2 KiB of fp8
@@ -415,7 +407,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_mfma_kernel(const ARGS args)
 
     // The first cached tiles are requested before anything else: page ids now, the copies (bf16 cache) as soon
     // as the ids are there, so that they travel while Q is loaded and rotated.
-    const int n_cache_keys = (MODE == MODE_SUFFIX) ? P : min(P, last_row / g + 1);
+    const int n_cache_keys = (MODE == MODE_SUFFIX) ? P : min(P, (t.row0 + t.n_rows - 1) / g + 1);
     const int n_kt = (n_cache_keys + BN - 1) / BN;
     // This wavefront's pages of tiles 0, 1, 2 come with the tile record; the steps take pg_v, of tile kt + 1, and pg_k, of tile
     // kt + 2.
@@ -427,6 +419,23 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_mfma_kernel(const ARGS args)
     };
     const int pg0 = of_wave(t.first_pages), pg1 = of_wave(t.first_pages + 4), pg2 = of_wave(t.first_pages + 8);
     int pg_v = pg1, pg_k = pg2;
+    auto first_copies = [&]() __attribute__((always_inline)) {
+        if (KV_FP8 || n_kt == 0) return;
+        fetch_cache(pg0, kbuf_of(0), pg0, vbuf_of(0));
+        if (n_kt > 1) fetch_cache(pg1, kbuf_of(1), 0, nullptr);
+    };
+    DraftRow draft = {0, 0, 0, 0, 0, 0};
+    if constexpr (DRAFT) {
+        first_copies();          // (they travel while the rows are found)
+        int tokens;
+        draft = draft_row<false>(a, __builtin_amdgcn_readfirstlane(t.sq_lo), __builtin_amdgcn_readfirstlane(t.sq_hi), (t.row0 + wave * 32 + n) / g, tokens);
+        t.n_rows = __builtin_amdgcn_readfirstlane(min(t.n_rows, tokens * g - t.row0));
+        if (t.n_rows <= 0) {
+            __builtin_amdgcn_s_waitcnt(0x0F70);          // (the LDS is the next workgroup's)
+            return;
+        }
+    }
+    const int last_row = t.row0 + t.n_rows - 1;
     float k_scale = 1.f, v_scale = 1.f;
     if (KV_FP8 && P > 0) {      // (nothing has written the scales of a cluster without cached keys)
         const float *sc = a.kv_scale + ((int64_t)cluster * a.n_layers + a.layer) * 2 * Hkv;
@@ -494,10 +503,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_mfma_kernel(const ARGS args)
     // and lane 31 of the last row block the maxima.
     const int lim_min = __builtin_amdgcn_readlane(lim[0], 0), lim_max = __builtin_amdgcn_readlane(lim[MI - 1], 31);
 
-    if (!KV_FP8 && n_kt > 0) {
-        fetch_cache(pg0, kbuf_of(0), pg0, vbuf_of(0));
-        if (n_kt > 1) fetch_cache(pg1, kbuf_of(1), 0, nullptr);
-    }
+    if constexpr (!DRAFT) first_copies();
     // ---- Q: load, rotate at position P + qpos (suffix) / qpos (prefix), keep as B operands ----
     // All loads of the phase (Q row halves, then the rotation table entries) are issued before any of them is
     // used, so the phase costs one memory round trip and not one per channel group.

@@ -18,16 +18,44 @@ constexpr int PART = kPageTokens * D * 2;       // one page's K (or V) of one he
 constexpr int CH = 2;                           // pages of own keys taken together
 constexpr int CB = 8;                           // 16-channel blocks of a head
 
-// Eight channels of a row of the caller's at c0 and c0 + 64, rotated.
-__device__ __forceinline__ void load_rotated(const uint16_t *row, int c0, const float2 *rope, float (&lo)[8], float (&hi)[8])
+// What a lane has of a row of the caller's (channels 32 i + 8 q .. + 7, two of the four i a rotation's halves of each other), as it comes, and
+// rotated: operand pieces, binary16.
+struct RawRow {
+    dec_u32x4 w[4];
+};
+__device__ __forceinline__ RawRow load_row(const uint16_t *row)
 {
-    dec_load8(row + c0, lo);
-    dec_load8(row + HALF + c0, hi);
-    if (rope)
+    RawRow r;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float2 cs = rope[c0 + i];
-            rotate_pair(lo[i], hi[i], cs.x, cs.y);
+    for (int i = 0; i < 4; ++i) r.w[i] = *reinterpret_cast<const dec_u32x4 *>(row + 32 * i);
+    return r;
+}
+// (cos, sin) of two channels each, of channels 8 q .. + 7 and 32 + 8 q .. + 7.
+struct Turns {
+    float4 cs[2][4];
+};
+__device__ __forceinline__ Turns load_turns(const float2 *rope)
+{
+    Turns t;
+#pragma unroll
+    for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t.cs[cb][e] = rope ? reinterpret_cast<const float4 *>(rope + 32 * cb)[e] : make_float4(1.f, 0.f, 1.f, 0.f);
+    return t;
+}
+__device__ __forceinline__ void rotate_row(const RawRow &r, const Turns &t, float scale, dec_u32x4 (&out)[4])
+{
+#pragma unroll
+    for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float a0 = __uint_as_float(r.w[cb][e] << 16), a1 = __uint_as_float(r.w[cb][e] & 0xFFFF0000u);
+            float b0 = __uint_as_float(r.w[cb + 2][e] << 16), b1 = __uint_as_float(r.w[cb + 2][e] & 0xFFFF0000u);
+            const float4 cs = t.cs[cb][e];
+            rotate_pair(a0, b0, cs.x, cs.y);
+            rotate_pair(a1, b1, cs.z, cs.w);
+            out[cb][e] = pack2_f16(a0 * scale, a1 * scale);
+            out[cb + 2][e] = pack2_f16(b0 * scale, b1 * scale);
         }
 }
 
@@ -71,7 +99,17 @@ __global__ void __launch_bounds__(256, 3) draft_own_kernel(const DraftArgs a)
         lse_q[i] = -INFINITY;
         if (q + 4 * i < a.n_splits) lse_q[i] = a.lse_cached[(q + 4 * i) * a.split_lse_elems + (int64_t)head * a.lse_stride + out_row];
     }
-    // keys of the first pages, on their way while rows and new keys are rotated
+    // Rows, new keys and values and the keys of the first pages are all asked for before any of them is used: one round trip.
+    const int tok = min(j, rows - 1);
+    const Turns q_turns = load_turns(a.rope ? a.rope + (int64_t)(base + jr) * HALF + 8 * q : nullptr);
+    const RawRow q_raw = load_row(static_cast<const uint16_t *>(a.q) + io + 8 * q), k_raw = load_row(kg + tok * kv_row + 8 * q);
+    uint32_t v_raw[CB][4];          // channel 16 cb + j of tokens 4 q .. 4 q + 3
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint16_t *vt = vg + min(4 * q + i, rows - 1) * kv_row + j;
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) v_raw[cb][i] = vt[16 * cb];
+    }
     const int n_pages = (n_old + kPageTokens - 1) / kPageTokens;
     dec_u32x4 ka[CH][4];
     auto load_keys = [&](int pg0) __attribute__((always_inline)) {
@@ -83,47 +121,28 @@ __global__ void __launch_bounds__(256, 3) draft_own_kernel(const DraftArgs a)
         }
     };
     if (n_pages > 0) load_keys(0);
+    __builtin_amdgcn_sched_barrier(0);
 
     // ---- the rows, as right operand: channels 32 cbk + 8 q .. + 7 of row j ----
     dec_f16x8 qb[4];
     {
-        const float scale = live ? a.scale_log2e : 0.f;
-        const float2 *rope = a.rope ? a.rope + (int64_t)(base + jr) * HALF : nullptr;
+        dec_u32x4 w[4];
+        rotate_row(q_raw, q_turns, live ? a.scale_log2e : 0.f, w);
 #pragma unroll
-        for (int cb = 0; cb < 2; ++cb) {
-            float lo[8], hi[8];
-            load_rotated(static_cast<const uint16_t *>(a.q) + io, 32 * cb + 8 * q, rope, lo, hi);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                qb[cb][e] = (_Float16)(lo[e] * scale);
-                qb[cb + 2][e] = (_Float16)(hi[e] * scale);
-            }
-        }
+        for (int i = 0; i < 4; ++i) qb[i] = __builtin_bit_cast(dec_f16x8, w[i]);
     }
     dec_f32x4 O[CB];
     float m_run, l_run = 0.f;
     // ---- the pass's new tokens: keys as left operand, token j, values of channel 16 cb + j of tokens 4 q .. 4 q + 3 (zero behind the last) ----
     {
-        const int tok = min(j, rows - 1);
         dec_u32x4 k_new[4];
-        const float2 *rope = a.rope ? a.rope + (int64_t)(base + tok) * HALF : nullptr;
-#pragma unroll
-        for (int cb = 0; cb < 2; ++cb) {
-            float lo[8], hi[8];
-            load_rotated(kg + tok * kv_row, 32 * cb + 8 * q, rope, lo, hi);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                k_new[cb][e] = pack2_f16(lo[2 * e], lo[2 * e + 1]);
-                k_new[cb + 2][e] = pack2_f16(hi[2 * e], hi[2 * e + 1]);
-            }
-        }
+        rotate_row(k_raw, load_turns(a.rope ? a.rope + (int64_t)(base + tok) * HALF + 8 * q : nullptr), 1.f, k_new);
         uint2 v_new[CB];
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
-            uint32_t v[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = 4 * q + i < rows ? vg[(4 * q + i) * kv_row + 16 * cb + j] : (uint16_t)0;
-            v_new[cb] = make_uint2(v[0] | v[1] << 16, v[2] | v[3] << 16);
+            for (int i = 0; i < 4; ++i) v_raw[cb][i] = 4 * q + i < rows ? v_raw[cb][i] : 0u;
+            v_new[cb] = make_uint2(v_raw[cb][0] | v_raw[cb][1] << 16, v_raw[cb][2] | v_raw[cb][3] << 16);
         }
         // into the pages, once per query and KV head
         if (sub == 0) {

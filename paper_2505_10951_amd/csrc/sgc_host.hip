@@ -753,6 +753,15 @@ void build_draft_tiles(sgc_plan *pl, int tile_rows)
                 }
         }
     pl->draft_row_tiles = n_row_tiles;
+    // Tiles of a cluster's last rows are the ones that a pass of few tokens leaves empty: they are dispatched last, or tiles with rows share compute
+    // units while others have none (10 prompts of 1024, 320 queries of up to 4: 60 against 69 us).  With one key range all tiles go in
+    // row order; with several only those of the last quarter are moved, for the others read the same keys at the same time
+    // (13 prompts of 8100: 146 us, in row order 156 us).
+    for (auto &l : lists)
+        std::stable_sort(l.begin(), l.end(), [&](const auto &x, const auto &y) {
+            const auto key = [&](const Tile &t) { return S == 1 ? t.row0 : (int64_t)t.row0 * 4 >= (t.sq_hi - t.sq_lo + 1) * per_query * 3 ? 1 : 0; };
+            return key(x.first) < key(y.first);
+        });
     size_t slots = 0;
     for (auto &l : lists) slots = std::max(slots, l.size());
     pl->ftiles.assign(slots * kXcd, Tile{});
