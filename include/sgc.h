@@ -286,8 +286,9 @@ int sgc_decode_step_batched_noalloc(sgc_ctx *ctx, const sgc_cache *cache, sgc_pl
  * Counts are read on the device, and held to the pages: rows from dev_rows[n] on, and rows that would lie at or behind max_new_tokens, are left as
  * they are, in dev_o, dev_lse and the pages alike; so are all rows of a query whose dev_done[n] is negative or dev_rows[n] below one.
  * The pass's results go by its own arguments and the pages alone: repeated with the same counts it gives the same bits.
- * dev_o and dev_lse may not overlap dev_q, dev_k or dev_v (SGC_EINVAL).  A value that is not finite among the pass's new tokens can turn that channel
- * of the query's other rows of the pass into NaN.  bf16 io, head_dim 128, as decode steps.
+ * dev_o and dev_lse may not overlap dev_q, dev_k or dev_v (SGC_EINVAL).  A value that is not finite, of the query's own tokens or new ones, leaves that channel of the rows that
+ * see it not finite (NaN or infinity), and all else as it is.  bf16 io, head_dim 128, as decode steps.  The ranges that long prompts are split into meet in a block of
+ * the plan: like all work of a context, its passes follow each other on one stream, captured and replayed ones among them.
  * Allocates nothing once the plan is uploaded and the rotary table covers its positions (max_position); where the tables are stale
  * the call refreshes them, except under capture (SGC_ESTATE).  Run the question's suffix prefill of every layer first (sgc_plan_upload where no query has question
  * tokens); move the counts on when the last layer is through. */
@@ -409,8 +410,8 @@ int sgc_project_out(sgc_ctx *ctx, const void *dev_o, const void *dev_w_o, int32_
  * Kp = d_model rounded up to 128 and zeros from d_model on, dev_exponents [ceil(n_features / 128)][Kp / 128].  Codes and exponents that come
  * from elsewhere may be used as they are if they are laid out so.  Once per weight.
  * sgc_project_fp8: dev_x: n_rows rows of d_model elements, x_stride elements apart, every row 16-byte aligned; dev_y: n_rows rows of
- * n_features elements, y_stride apart, aligned to their type; nothing between or behind the rows is touched.  n_features: any; d_model: a
- * multiple of 16.  x_dtype and y_dtype: SGC_F32 or SGC_BF16.  dev_workspace: sgc_project_fp8_workspace bytes, 16-byte aligned, contents of no meaning before and
+ * n_features elements, y_stride apart, aligned to their type; nothing between or behind the rows is touched.  n_rows up to 2^23; n_features: any; d_model: a
+ * multiple of 16, up to 2^20.  x_dtype and y_dtype: SGC_F32 or SGC_BF16.  dev_workspace: sgc_project_fp8_workspace bytes, 16-byte aligned, contents of no meaning before and
  * after.  dev_y may not overlap dev_x.  The order of the sums follows from the sizes: the same call gives the same bits.  ctx may be NULL (both). */
 int sgc_quantise_weight_fp8(sgc_ctx *ctx, const void *dev_w, int32_t w_dtype, int32_t n_features, int32_t d_model, void *dev_codes,
                             void *dev_exponents, void *hip_stream);

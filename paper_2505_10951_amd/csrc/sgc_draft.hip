@@ -4,6 +4,8 @@
 // rest: the query's own keys, the pass's new ones among them, the sum of all parts, and the new keys' way into the query's pages.
 #include <hip/hip_runtime.h>
 
+#include <atomic>
+
 #include "sgc_draft_rows.h"
 #include "sgc_own_keys.h"
 
@@ -178,9 +180,31 @@ __global__ void __launch_bounds__(256, 3) draft_own_kernel(const DraftArgs a)
             l_run += dec_bf16_to_f32(b);
             w[r] = (short)b;
         }
+        uint32_t most = 0;
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb)
-            O[cb] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(draft_s16x4, v_new[cb]), w, dec_f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) most = max(most, v_raw[cb][i] & 0x7FFFu);
+        if (!__any(most >= 0x7F80u)) {
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb)
+                O[cb] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(draft_s16x4, v_new[cb]), w, dec_f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+        } else {
+            // A value that is not finite, times the weight 0 of a row that does not see it, would be NaN: tokens one by one, and rows that do
+            // not see one are left as they are.
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) O[cb] = dec_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+            for (int t = 0; t < rows; ++t)
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb) {
+                    const int at = t - 4 * q;
+                    const uint2 v = make_uint2(v_new[cb].x & (at == 0 ? 0xFFFFu : at == 1 ? 0xFFFF0000u : 0u), v_new[cb].y & (at == 2 ? 0xFFFFu : at == 3 ? 0xFFFF0000u : 0u));
+                    const dec_f32x4 one = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(draft_s16x4, v), w, dec_f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) O[cb][r] = t <= jr ? O[cb][r] + one[r] : O[cb][r];
+                }
+        }
     }
     // ---- the keys in the pages, online ----
     auto v_off = [&](int cb) { return ((((cb >> 1) * 2 + (q & 1)) * 32 + (cb & 1) * 16 + j) * 16) + 8 * (q >> 1); };
@@ -312,6 +336,7 @@ typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
 
 constexpr int FW = 8, SLOT = 32 * D * 4;        // wavefronts, and a wavefront's part of the 32 rows
 constexpr int FEW_LDS = FW * SLOT + FW * 32 * 8 + 32 * 8 + 16;
@@ -619,10 +644,10 @@ __global__ void __launch_bounds__(FW * 64, 2) draft_few_kernel(const AttnArgs a)
             x = unit_at(u + FW);
             load_keys(x);
         }
+        const int sees = !valid || row.sq != now.sq ? 0 : now.kind == OWN ? now.left : min(now.left, row.j + 1);          // (own and new keys)
         if (now.kind != CACHED) {
             const float ratio = KV_FP8 ? 1.0f / k_scale : 1.0f;          // (own keys are not quantised)
-            // (of the lane's keys: their 4 h is taken off what the row sees, so that each is compared with a constant)
-            const int see = (!valid || row.sq != now.sq ? 0 : now.kind == OWN ? now.left : min(now.left, row.j + 1)) - 4 * h;
+            const int see = sees - 4 * h;          // (of the lane's keys, so that each is compared with a constant)
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) < see ? s[r] * ratio : -INFINITY;
         } else if (now.left < 32) {
@@ -676,6 +701,39 @@ __global__ void __launch_bounds__(FW * 64, 2) draft_few_kernel(const AttnArgs a)
                     const int tok = (i >> 2) * kPageTokens + 2 * (e & 1) + 8 * (e >> 1);
                     vf[i][e] &= tok + 1 < there ? 0xFFFFFFFFu : tok < there ? 0xFFFFu : 0u;
                 }
+        }
+        if (now.kind != CACHED) {
+            u16x2 most = {0, 0};
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, vf[i][e] & 0x7FFF7FFFu));
+            if (__builtin_expect(__any(most[0] >= 0x7F80 || most[1] >= 0x7F80), 0)) {
+                // A value that is not finite, times the weight 0 of a row that does not see it, would be NaN.  Such values are taken out, and
+                // counted for every row that sees them: where there is one, the channel is NaN.
+#pragma unroll
+                for (int db = 0; db < 4; ++db) {
+                    f32x16 met;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) met[r] = 0.f;
+#pragma unroll
+                    for (int pg = 0; pg < 2; ++pg) {
+                        u32x4 bad, seen;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t v = vf[4 * pg + db][e];
+                            const uint32_t b = ((v & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((v & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+                            vf[4 * pg + db][e] = v & ~b;
+                            bad[e] = b & 0x3F803F80u;          // (ones)
+                            const int tok = pg * kPageTokens + 4 * h + 2 * (e & 1) + 8 * (e >> 1);
+                            seen[e] = tok + 1 < sees ? 0x3F803F80u : tok < sees ? 0x3F80u : 0u;
+                        }
+                        met = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, bad), __builtin_bit_cast(bf16x8, seen), met, 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) oacc[db][r] = met[r] > 0.f ? __builtin_nanf("") : oacc[db][r];
+                }
+            }
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -801,14 +859,14 @@ __global__ void __launch_bounds__(FW * 64, 2) draft_few_kernel(const AttnArgs a)
 
 hipError_t launch_draft_few(const AttnArgs &a, hipStream_t s)
 {
-    static bool configured = false;     // raise the dynamic LDS limit once
+    static std::atomic<bool> configured{false};          // raise the dynamic LDS limit once
     auto kern = a.pool.kv_dtype == SGC_FP8_E4M3 ? draft_few_kernel<true> : draft_few_kernel<false>;
-    if (!configured) {
+    if (!configured.load(std::memory_order_acquire)) {
         for (const void *f : {reinterpret_cast<const void *>(draft_few_kernel<true>), reinterpret_cast<const void *>(draft_few_kernel<false>)}) {
             const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, FEW_LDS);
             if (e != hipSuccess) return e;
         }
-        configured = true;
+        configured.store(true, std::memory_order_release);
     }
     if (a.n_tiles <= 0) return hipSuccess;
     hipLaunchKernelGGL(kern, dim3(a.n_tiles), dim3(FW * 64), FEW_LDS, s, a);

@@ -13,6 +13,8 @@
 // 16-bit instruction, whose sums keep 24 bits (8e-8), at half the rate.
 #include <hip/hip_runtime.h>
 
+#include <atomic>
+
 #include <algorithm>
 #include <type_traits>
 
@@ -611,23 +613,23 @@ __global__ void __launch_bounds__(256, 1) project_fp8_big_kernel(const Fp8Args a
         }
 }
 
-template <class K>
-hipError_t launch_lds(K kern, int64_t blocks, size_t lds, const Fp8Args &a, hipStream_t s)
+template <auto KERN>
+hipError_t launch_lds(int64_t blocks, size_t lds, const Fp8Args &a, hipStream_t s)
 {
-    static const void *configured = nullptr;          // (per kernel type; raised once per kernel)
-    if (lds > 65536 && configured != reinterpret_cast<const void *>(kern)) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    static std::atomic<bool> configured{false};          // raise the dynamic LDS limit once a kernel
+    if (lds > 65536 && !configured.load(std::memory_order_acquire)) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(KERN), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return e;
-        configured = reinterpret_cast<const void *>(kern);
+        configured.store(true, std::memory_order_release);
     }
-    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(256), lds, s, a);
+    hipLaunchKernelGGL(KERN, dim3((unsigned)blocks), dim3(256), lds, s, a);
     return hipGetLastError();
 }
 int64_t tiles_of(const Fp8Args &a, int tm, int tn) { return ((a.M + tm - 1) / tm * ((a.N + tn - 1) / tn) + 7) / 8 * 8; }
 template <class T>
 hipError_t launch_tile(const Fp8Args &a, hipStream_t s)
 {
-    return launch_lds(project_fp8_tile_kernel<T>, tiles_of(a, T::TM, T::TN), T::LDS, a, s);
+    return launch_lds<project_fp8_tile_kernel<T>>(tiles_of(a, T::TM, T::TN), T::LDS, a, s);
 }
 // Tiles, with as many of their steps as LDS holds.
 typedef Tile<64, 64, 8, false> T64;
@@ -649,7 +651,7 @@ struct Choice {
     float step;
     hipError_t (*launch)(const Fp8Args &, hipStream_t);
 };
-hipError_t launch_big(const Fp8Args &a, hipStream_t s) { return launch_lds(project_fp8_big_kernel, tiles_of(a, 256, 256), BIG_LDS, a, s); }
+hipError_t launch_big(const Fp8Args &a, hipStream_t s) { return launch_lds<project_fp8_big_kernel>(tiles_of(a, 256, 256), BIG_LDS, a, s); }
 constexpr Choice kTiles[] = {{64, 64, 0.25f, launch_tile<T64>},    {64, 128, 0.40f, launch_tile<T64W>},  {128, 128, 0.53f, launch_tile<T128>},
                              {192, 128, 0.78f, launch_tile<T192>}, {256, 128, 0.98f, launch_tile<T256>}, {256, 256, 1.45f, launch_big}};
 constexpr Choice kTilesF32[] = {{64, 64, 0.42f, launch_tile<F64>}, {64, 128, 0.50f, launch_tile<F64W>}, {128, 128, 0.72f, launch_tile<F128>}};
