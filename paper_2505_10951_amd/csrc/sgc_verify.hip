@@ -16,9 +16,16 @@ namespace {
 // Four (eight) neighbouring elements of a row that starts at any element: rows of odd lengths follow each other.
 struct __attribute__((packed, aligned(4))) Row4 {
     float x[4];
+    __device__ __forceinline__ float get(int e) const { return x[e]; }
+    __device__ __forceinline__ void set(int e, float v) { x[e] = v; }
+    __device__ __forceinline__ void renew() { asm volatile("" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3])); }
 };
+// (by words: as eight 16-bit numbers they would take a register each)
 struct __attribute__((packed, aligned(2))) Row8 {
-    uint16_t x[8];
+    uint32_t w[4];
+    __device__ __forceinline__ float get(int e) const { return __uint_as_float(e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16); }
+    __device__ __forceinline__ void set(int e, uint16_t v) { w[e >> 1] = e & 1 ? (w[e >> 1] & 0xFFFFu) | (uint32_t)v << 16 : (w[e >> 1] & 0xFFFF0000u) | v; }
+    __device__ __forceinline__ void renew() { asm volatile("" : "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3])); }
 };
 
 template <typename T>
@@ -57,6 +64,38 @@ __device__ __forceinline__ Part join(const Part &a, const Part &b, float c)
 
 constexpr int PT = 512;           // threads of a workgroup
 
+// Over the 64 lanes, result in all of them: within 16 by the data-parallel crossbar, then across by lane swaps (a shuffle through LDS takes ten
+// times as long, and a row's kernel is little else than such steps where there are few).
+template <typename V, typename F>
+__device__ __forceinline__ V over_lanes(V x, F f)
+{
+    auto from = [&](auto ctrl) __attribute__((always_inline)) { return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xF, 0xF, false)); };
+    x = f(x, from(std::integral_constant<int, 0xB1>{}));           // lane ^ 1
+    x = f(x, from(std::integral_constant<int, 0x4E>{}));           // lane ^ 2
+    x = f(x, from(std::integral_constant<int, 0x141>{}));          // the other four of eight
+    x = f(x, from(std::integral_constant<int, 0x140>{}));          // the other eight of sixteen
+    const auto a = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    x = f(__builtin_bit_cast(V, (uint32_t)a[0]), __builtin_bit_cast(V, (uint32_t)a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    return f(__builtin_bit_cast(V, (uint32_t)b[0]), __builtin_bit_cast(V, (uint32_t)b[1]));
+}
+// The lanes' parts put together: the largest of all first, then what each adds to its sum.
+__device__ __forceinline__ Part over_lanes(const Part &mine, float c)
+{
+    Part r;
+    r.top = over_lanes(mine.top, [](float a, float b) { return fmaxf(a, b); });
+    r.at = over_lanes(mine.top == r.top ? mine.at : 0x7fffffff, [](int a, int b) { return min(a, b); });
+    r.sum = over_lanes(mine.sum > 0.f ? mine.sum * weight(mine.top, r.top, c) : 0.f, [](float a, float b) { return a + b; });
+    return r;
+}
+
+// The wavefronts' parts, one to a lane.
+__device__ __forceinline__ Part part_of(const Part *part, int n)
+{
+    const int lane = threadIdx.x & 63;
+    return lane < n ? part[lane] : Part{-INFINITY, 0.f, 0x7fffffff};
+}
+
 // Elements [lo, hi) of a row, all threads: f(first index, values, how many)
 template <typename T, typename F>
 __device__ __forceinline__ void over_row(const T *row, int lo, int hi, F f)
@@ -67,7 +106,7 @@ __device__ __forceinline__ void over_row(const T *row, int lo, int hi, F f)
         if (i + N <= hi) {
             const typename RowOf<T>::vec v = *reinterpret_cast<const typename RowOf<T>::vec *>(row + i);
 #pragma unroll
-            for (int e = 0; e < N; ++e) x[e] = logit(RowOf<T>::value(v.x[e]));
+            for (int e = 0; e < N; ++e) x[e] = logit(v.get(e));
         } else {
 #pragma unroll
             for (int e = 0; e < N; ++e) x[e] = i + e < hi ? logit(RowOf<T>::value(row[i + e])) : -INFINITY;
@@ -110,20 +149,11 @@ __global__ void __launch_bounds__(PT) token_probs_kernel(const T *logits, int64_
     } else {
         for (int k = (int)threadIdx.x & 63; k < chunks; k += 64) mine = join(mine, parts[r * chunks + k], c);      // (every wavefront the same)
     }
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        Part other;
-        other.top = __shfl_xor(mine.top, d);
-        other.sum = __shfl_xor(mine.sum, d);
-        other.at = __shfl_xor(mine.at, d);
-        mine = join(mine, other, c);
-    }
+    mine = over_lanes(mine, c);
     if (STATS) {
         if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = mine;
         __syncthreads();
-        mine = part[0];
-#pragma unroll
-        for (int w = 1; w < PT / 64; ++w) mine = join(mine, part[w], c);
+        mine = over_lanes(part_of(part, PT / 64), c);
         if (!WRITE) {
             if (threadIdx.x == 0) parts[r * chunks + chunk] = mine;
             return;
@@ -164,60 +194,65 @@ __global__ void __launch_bounds__(RT) token_probs_row_kernel(const T *logits, in
     const T *row = logits + r * logits_stride;
     float *out = probs + r * probs_stride;
     // (a thread's first token: the workgroup's pieces begin at 128-byte lines of the output, up to 31 tokens in front of the row)
-    const int first = (int)threadIdx.x * N - (int)((reinterpret_cast<uintptr_t>(out) >> 2) & 31);
+    int first = (int)threadIdx.x * N - (int)((reinterpret_cast<uintptr_t>(out) >> 2) & 31);
+    // Every load is a whole vector inside the row and none is in a branch, where each would be waited for by itself: one that begins
+    // in front of the row or reaches behind it is moved inside, and what its neighbour has as well is ruled out.
+    auto inside = [&](int i) __attribute__((always_inline)) { return min(max(i, 0), vocab - N); };
     vec v[NV];
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        const int i = first + k * RT * N;
-        if (i >= 0 && i + N <= vocab) {
-            v[k] = *reinterpret_cast<const vec *>(row + i);
-        } else {
+    for (int k = 0; k < NV; ++k) v[k] = *reinterpret_cast<const vec *>(row + inside(first + k * RT * N));
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int e = 0; e < N; ++e) v[k].x[e] = i + e >= 0 && i + e < vocab ? row[i + e] : RowOf<T>::ruled_out();
-        }
+    for (int k = 0; k < NV; ++k) {
+        const int i = first + k * RT * N, shift = inside(i) - i;
+        if (__any(shift != 0))
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (shift + e < 0 || shift + e >= N) v[k].set(e, RowOf<T>::ruled_out());
     }
-    auto x = [&](int k, int e) __attribute__((always_inline)) { return logit(RowOf<T>::value(v[k].x[e])); };
+    auto x = [&](int k, int e) __attribute__((always_inline)) { return logit(v[k].get(e)); };
+    // (between the passes over the registers: nothing that one worked out is kept for the next, for which there is no room)
+    auto renew = [&]() __attribute__((always_inline)) {
+        asm volatile("" : "+v"(first));
+#pragma unroll
+        for (int k = 0; k < NV; ++k) v[k].renew();
+    };
     Part mine = {-INFINITY, 0.f, 0x7fffffff};
 #pragma unroll
     for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int e = 0; e < N; ++e) mine.top = fmaxf(mine.top, x(k, e));
+    renew();
     if (mine.top > -INFINITY) {
         if (c == 0.f) {
 #pragma unroll
             for (int k = NV - 1; k >= 0; --k)
 #pragma unroll
                 for (int e = N - 1; e >= 0; --e)
-                    if (x(k, e) == mine.top) mine.at = first + k * RT * N + e;
+                    if (x(k, e) == mine.top) mine.at = inside(first + k * RT * N) + e;
         } else {
 #pragma unroll
-            for (int k = 0; k < NV; ++k)
+            for (int k = 0; k < NV; ++k) {
 #pragma unroll
                 for (int e = 0; e < N; ++e) mine.sum += weight(x(k, e), mine.top, c);
+                __builtin_amdgcn_sched_barrier(0);          // (vector by vector: widened all at once they would not fit)
+            }
         }
     }
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        Part other;
-        other.top = __shfl_xor(mine.top, d);
-        other.sum = __shfl_xor(mine.sum, d);
-        other.at = __shfl_xor(mine.at, d);
-        mine = join(mine, other, c);
-    }
+    mine = over_lanes(mine, c);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = mine;
     __syncthreads();
-    mine = part[0];
-#pragma unroll
-    for (int w = 1; w < RT / 64; ++w) mine = join(mine, part[w], c);
+    renew();
+    mine = over_lanes(part_of(part, RT / 64), c);
     const bool some = mine.top > -INFINITY;
     const float inv = some ? 1.f / mine.sum : 0.f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-        const int i = first + k * RT * N;
+        const int want = first + k * RT * N, i = inside(want);
         float p[N];
 #pragma unroll
         for (int e = 0; e < N; ++e) p[e] = c == 0.f ? (some && i + e == mine.at ? 1.f : 0.f) : (some ? weight(x(k, e), mine.top, c) * inv : 0.f);
-        if (i >= 0 && i + N <= vocab) {
+        if (i == want) {
 #pragma unroll
             for (int q = 0; q < N / 4; ++q) {
                 Row4 y;
@@ -228,22 +263,29 @@ __global__ void __launch_bounds__(RT) token_probs_row_kernel(const T *logits, in
         } else {
 #pragma unroll
             for (int e = 0; e < N; ++e)
-                if (i + e >= 0 && i + e < vocab) out[i + e] = p[e];
+                if (i + e >= want && i + e < want + N) out[i + e] = p[e];
         }
+        __builtin_amdgcn_sched_barrier(0);
     }
 }
 
 // Vectors of a thread that hold a row, or 0: the row does not fit, and is read twice.
 int row_vectors(int64_t vocab, bool f32)
 {
+    if (vocab < 8) return 0;          // (not a vector long)
     const int64_t n = (vocab + 31 + RT * (f32 ? 4 : 8) - 1) / (RT * (f32 ? 4 : 8));
-    return n <= 2 ? 2 : n <= 4 ? 4 : n <= 8 ? 8 : n <= 13 ? 13 : n <= 16 ? 16 : 0;
+    return n <= 1 ? 1 : n <= 2 ? 2 : n <= 4 ? 4 : n <= 8 ? 8 : n <= 13 ? 13 : n <= 16 ? 16 : n <= 20 ? 20 : 0;
 }
+// How many workgroups a row is dealt to, at most.
 int probs_chunks(int64_t rows, int64_t vocab)
 {
     const int64_t want = (512 + rows - 1) / std::max<int64_t>(rows, 1);
     return (int)std::max<int64_t>(1, std::min<int64_t>({want, (vocab + 4095) / 4096, 64}));
 }
+// Whether it is one, which reads the row once into registers: where the row fits, and is short or one of many.  us, one / several: 32-bit logits,
+// 1 x 8000 3.9 / 6.4, 20 x 16000 5.6 / 7.0, 20 x 32000 8.3 / 7.5, 40 x 32000 8.7 / 9.5, 40 x 50021 12.6 / 11.2, 80 x 50021 13.8 / 16.0,
+// 160 x 64000 23 / 32; 16 bits, 20 x 16000 5.8 / 6.6, 40 x 50021 15.3 / 11.9, 80 x 64000 16.6 / 18.3, 80 x 131072 36 / 31, 160 x 131072 44 / 46.
+bool probs_in_registers(int64_t rows, int64_t vocab, bool f32) { return row_vectors(vocab, f32) > 0 && (vocab <= 16384 || rows * 1000 >= vocab); }
 template <typename T, int NV>
 void launch_rows(const T *x, int64_t xs, float *p, int64_t ps, int64_t rows, int vocab, float c, hipStream_t s)
 {
@@ -582,7 +624,8 @@ int sgc_token_probs(sgc_ctx *ctx, int64_t n_rows, int32_t vocab, const void *dev
     const uintptr_t eb = logits_dtype == SGC_F32 ? 4 : 2;
     if (!dev_logits || !dev_probs) return report(ctx, SGC_EINVAL, "dev_logits / dev_probs is NULL");
     if (reinterpret_cast<uintptr_t>(dev_logits) % eb || reinterpret_cast<uintptr_t>(dev_probs) % 4) return report(ctx, SGC_EINVAL, "an array is not aligned to its element type");
-    const int chunks = probs_chunks(n_rows, vocab);
+    const bool in_registers = probs_in_registers(n_rows, vocab, logits_dtype == SGC_F32);
+    const int chunks = in_registers ? 1 : probs_chunks(n_rows, vocab);
     const size_t need = sgc_token_probs_workspace(n_rows, vocab);
     if (need > 0 && (!dev_workspace || workspace_bytes < need || reinterpret_cast<uintptr_t>(dev_workspace) % 16))
         return report(ctx, SGC_EINVAL, "the workspace has to hold %zu bytes, 16-byte aligned", need);
@@ -594,8 +637,10 @@ int sgc_token_probs(sgc_ctx *ctx, int64_t n_rows, int32_t vocab, const void *dev
         const T *x = static_cast<const T *>(dev_logits) + first * logits_stride;
         float *p = dev_probs + first * probs_stride;
         const dim3 grid((unsigned)chunks, (unsigned)rows);
-        const int nv = chunks == 1 ? row_vectors(vocab, logits_dtype == SGC_F32) : 0;
-        if (nv == 2) {
+        const int nv = in_registers ? row_vectors(vocab, logits_dtype == SGC_F32) : 0;
+        if (nv == 1) {
+            launch_rows<T, 1>(x, logits_stride, p, probs_stride, rows, vocab, c, s);
+        } else if (nv == 2) {
             launch_rows<T, 2>(x, logits_stride, p, probs_stride, rows, vocab, c, s);
         } else if (nv == 4) {
             launch_rows<T, 4>(x, logits_stride, p, probs_stride, rows, vocab, c, s);
@@ -605,6 +650,8 @@ int sgc_token_probs(sgc_ctx *ctx, int64_t n_rows, int32_t vocab, const void *dev
             launch_rows<T, 13>(x, logits_stride, p, probs_stride, rows, vocab, c, s);
         } else if (nv == 16) {
             launch_rows<T, 16>(x, logits_stride, p, probs_stride, rows, vocab, c, s);
+        } else if (nv == 20) {
+            launch_rows<T, 20>(x, logits_stride, p, probs_stride, rows, vocab, c, s);
         } else if (chunks == 1) {
             hipLaunchKernelGGL((token_probs_kernel<T, true, true>), grid, dim3(PT), 0, s, x, logits_stride, p, probs_stride, vocab, c, nullptr, 1);
         } else {
