@@ -683,8 +683,8 @@ void build_decode_tiles(sgc_plan *pl, int tile_rows)
 // Row tiles of passes over drafted tokens: max_rows x g rows per query at most, all queries of a (cluster, KV head) stacked, the keys of
 // every row tile split into S ranges.
 // One launch (draft_few_kernel) where a cluster and KV head have few rows; its tiles are 32 rows, over cached and own keys alike.
-// Two otherwise: 128 rows over the cached keys, whose ranges are dealt as for decode steps, and long ones cut into at most 48 steps of 64 keys, so that
-// tiles that end up without rows leave no compute unit idle (64 queries of up to 8 tokens, 64 heads, prompts of 16384: S = 2, 4, 6, 8 239, 219, 217, 211 us).
+// Two otherwise: 128 rows over the cached keys, whose ranges are dealt as for decode steps, and long ones cut into at most 64 steps of 64 keys, so that
+// tiles that end up without rows leave no compute unit idle (64 queries of up to 8 tokens, 64 heads, prompts of 16384: S = 1, 2, 4, 6, 8 309, 226, 199, 210, 206 us).
 void build_draft_tiles(sgc_plan *pl, int tile_rows)
 {
     const sgc_ctx *ctx = pl->ctx;
@@ -726,7 +726,7 @@ void build_draft_tiles(sgc_plan *pl, int tile_rows)
     if (pl->draft_few) S = few_splits;
     else if (row_tiles > 0) {
         const int64_t full = std::min(max_steps / 8, std::max<int64_t>(512 / row_tiles, 1)), half = std::min({max_steps / 3, std::max<int64_t>(256 / row_tiles, 1), (int64_t)8});
-        S = (int)std::min<int64_t>(kDecodeMaxSplits, std::max({(int64_t)1, full, half, std::min<int64_t>((max_steps + 47) / 48, 8)}));
+        S = (int)std::min<int64_t>(kDecodeMaxSplits, std::max({(int64_t)1, full, half, std::min<int64_t>((max_steps + 63) / 64, 8)}));
     }
     if (max_steps >= (1 << 24) / 64) S = 1;      // the position offset travels in 24 bits of the tile record
     pl->draft_splits = S;
