@@ -211,7 +211,8 @@ __device__ __forceinline__ const AttnArgs &attn_args(const ARGS &c) { return c.a
 //
 // ARGS: AttnArgs, or CarriedSuffix / CarriedPrefix, whose tables are read where they arrive, among the launch's arguments.
 //
-// DRAFT: a pass over drafted tokens.  A tile's rows are numbered through the tokens that the cluster's queries bring to this pass, whose
+// DRAFT: a pass over drafted tokens (320 queries of up to 4, ten prompts of 1024: 26 us, 37 with likely empty tiles among the others and the first copies
+// behind the search for the rows; 64 queries of up to 8, 64 heads, fp8 prompts of up to 16384: 170 us of 200).  A tile's rows are numbered through the tokens that the cluster's queries bring to this pass, whose
 // counts are on the device; tiles behind the last of them end at once.  The cached keys alone, key ranges in fp32.
 template <bool KV_FP8, int MODE, bool QK8, bool OWN_RAW, typename ARGS, bool DRAFT = false>
 __global__ void __launch_bounds__(NW * 64, 2) attn_mfma_kernel(const ARGS args)

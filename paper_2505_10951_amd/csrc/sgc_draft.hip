@@ -1,7 +1,8 @@
 // Passes over drafted tokens (SubGCache arXiv 2505.10951, Sec. 3.4: every query of a cluster reuses the cluster's cached prompt;
 // App. A.2: up to 32 generated tokens per query): up to 16 new tokens of every query at once, each query at a position of its own.
-// The cached prompt is the 128-row kernel's work (sgc_attn_mfma.hip), rows = (query, drafted token, head of the group); here is the
-// rest: the query's own keys, the pass's new ones among them, the sum of all parts, and the new keys' way into the query's pages.
+// A pass of few rows is one launch, draft_few_kernel.  Of one of many, the cached prompt is the 128-row kernel's work (sgc_attn_mfma.hip), rows =
+// (query, drafted token, head of the group), and draft_own_kernel does the rest: the query's own keys, the pass's new ones among them, the sum of
+// all parts, and the new keys' way into the query's pages.
 #include <hip/hip_runtime.h>
 
 #include <atomic>
@@ -67,7 +68,9 @@ __device__ __forceinline__ void rotate_row(const RawRow &r, const Turns &t, floa
 // product's right operand (two pages to a 32-key product; the new tokens, one page of their own that is never read from memory, to a
 // 16-key one).  The new tokens' keys and values are taken from the caller's arrays: the pages they go to are read by other
 // wavefronts of the launch, which leave out everything behind the keys that were there before.
-// Bounded by the chain of dependent loads: counts -> keys -> values, a chunk of two pages to a round trip.
+// Bounded by the chain of dependent loads under a full memory: counts -> rows, new tokens and keys -> values, a chunk of two pages to a round trip -> partial
+// results.  320 queries of up to 4 tokens, 8 heads, 53 own keys on average, one key range: 26 us for 85 MB, 3.3 TB/s (28 us with the new
+// tokens asked for behind the rotated rows; values a chunk ahead as well: registers spill, 33 us).  64 queries of 8 heads, four ranges: 34 us.
 __global__ void __launch_bounds__(256, 3) draft_own_kernel(const DraftArgs a)
 {
     const int lane = threadIdx.x & 63, j = lane & 15, q = lane >> 4;
@@ -329,7 +332,9 @@ __global__ void __launch_bounds__(256, 3) draft_own_kernel(const DraftArgs a)
 // row is put together from eight parts in LDS, and from the S ranges by the one that ends last.
 // Operands come straight from memory to registers: pages hold them in the order that v_mfma_f32_32x32x16 reads (S^T = K Q^T, O^T = V^T P^T: lane
 // (n, h) = (lane % 32, lane / 32) owns row n, as in the 128-row kernel).  The next unit's keys are asked for as soon as this one's
-// scores are formed, its values behind the second product.  Bounded by round trips, and past some units a wavefront by L2.
+// scores are formed, its values behind the second product.  Bounded by round trips: tile record, counts, rows, a unit each, the merge; past some units a
+// wavefront by what a compute unit takes in.  One query of 5 tokens, 8 KV heads, prompt of 411: 13.7 us (14.4 with 7 registers more of the new tokens'
+// operands held from the start); 5 queries over 3001 tokens in six ranges 20.6 us; two launches 20.8 and 30.3.
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
