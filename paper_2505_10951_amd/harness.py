@@ -275,6 +275,8 @@ class Fp8Weight:
     """A projection's weight [n_features][d_model] as e4m3 codes with a power-of-two scale per 128 x 128 block."""
 
     def __init__(self, w: torch.Tensor):
+        if not w.is_contiguous():
+            raise ValueError("the weight has to be contiguous")
         self.n_features, self.d_model = w.shape
         kb = -(-self.d_model // 128)
         self.codes = torch.empty((self.n_features, kb * 128), dtype=torch.uint8, device=w.device)
@@ -309,8 +311,10 @@ class DraftPass:
 
     def project(self, x: torch.Tensor, w: Fp8Weight, y: torch.Tensor) -> None:
         types = {torch.float32: sgc.SGC_F32, torch.bfloat16: sgc.SGC_BF16}
-        sgc.sgc_project_fp8(None, x.data_ptr(), types[x.dtype], x.shape[1], x.shape[0], w.codes.data_ptr(), w.exponents.data_ptr(), w.n_features,
-                            w.d_model, y.data_ptr(), types[y.dtype], y.shape[1], self.workspace.data_ptr(), self.workspace.numel(),
+        if x.stride(1) != 1 or y.stride(1) != 1 or tuple(x.shape) != (y.shape[0], w.d_model) or y.shape[1] != w.n_features:
+            raise ValueError(f"x {tuple(x.shape)} and y {tuple(y.shape)} do not go with a weight of {w.n_features} x {w.d_model}, or their rows are no rows")
+        sgc.sgc_project_fp8(None, x.data_ptr(), types[x.dtype], x.stride(0), x.shape[0], w.codes.data_ptr(), w.exponents.data_ptr(), w.n_features,
+                            w.d_model, y.data_ptr(), types[y.dtype], y.stride(0), self.workspace.data_ptr(), self.workspace.numel(),
                             torch.cuda.current_stream().cuda_stream)
 
 

@@ -418,7 +418,7 @@ def test_passes_through_a_layer_and_the_head():
             h = bf(_quantised_rows(bf(o[-R:].reshape(R, -1))) @ deq[3].T)
             ref = _quantised_rows(h) @ deq[4].T
             got = logits.reshape(n, R, V)[m]
-            # bf16 rounding of q, k, v, o, h (2^-9 each, amplified by the attention), and codes that take their neighbour (up to 2^-4
+            # bf16 rounding of q, k, v, o, h (2^-8 at most each, amplified by the attention), and codes that take their neighbour (up to 2^-4
             # of an element, on few of them): a few percent of the logits' spread
             assert np.linalg.norm(got - ref) <= 0.05 * np.linalg.norm(ref), (i, m, np.linalg.norm(got - ref) / np.linalg.norm(ref))
             a = int(accepted[m])
