@@ -429,7 +429,8 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_mfma_kernel(const ARGS args)
     if constexpr (DRAFT) {
         first_copies();          // (they travel while the rows are found)
         int tokens;
-        draft = draft_row<false>(a, __builtin_amdgcn_readfirstlane(t.sq_lo), __builtin_amdgcn_readfirstlane(t.sq_hi), (t.row0 + wave * 32 + n) / g, tokens);
+        draft = draft_row<false, true>(a, __builtin_amdgcn_readfirstlane(t.sq_lo), __builtin_amdgcn_readfirstlane(t.sq_hi), t.row0 / g, (t.row0 + NW * 32 - 1) / g,
+                                 (t.row0 + wave * 32 + n) / g, tokens);
         t.n_rows = __builtin_amdgcn_readfirstlane(min(t.n_rows, tokens * g - t.row0));
         if (t.n_rows <= 0) {
             __builtin_amdgcn_s_waitcnt(0x0F70);          // (the LDS is the next workgroup's)

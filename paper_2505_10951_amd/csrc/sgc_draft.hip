@@ -473,7 +473,7 @@ __global__ void __launch_bounds__(FW * 64, 2) draft_few_kernel(const AttnArgs a)
     // ---- the lane's row, and what its query has ----
     int tokens;
     const int r_all = t.row0 + n;
-    const DraftRow row = draft_row<true>(a, t.sq_lo, t.sq_hi, r_all / g, tokens);
+    const DraftRow row = draft_row<true, false>(a, t.sq_lo, t.sq_hi, 0, 0, r_all / g, tokens);
     const int rows = min(32, tokens * g - t.row0);
     if (rows <= 0) return;
     const bool valid = n < rows;
