@@ -488,8 +488,8 @@ __device__ __forceinline__ void answer(const VerifyArgs &a, int64_t n, const Dra
 }
 
 // The draw goes down the row by sums in 64 bits, of parts that get smaller: the token is the first at which the running sum is beyond u times the whole.
-// Many queries: one workgroup a query (320 queries, 50021 tokens, with the drafts' probabilities: 30 us, 128 MB at 4.2 TB/s; bounded by the compute
-// units that have two).  16 wavefronts sum a segment each; the segment that u falls into is looked through token by token.
+// Short rows: one workgroup a query.  8 wavefronts sum a segment each; the segment that u falls into is looked through token by token.
+// Bounded by the chain of its sums (313 queries of 315 tokens 7.8 us).
 constexpr int VT = 512, VW = VT / 64;
 __global__ void __launch_bounds__(VT, 4) verify_kernel(const VerifyArgs a)
 {
@@ -518,8 +518,9 @@ __global__ void __launch_bounds__(VT, 4) verify_kernel(const VerifyArgs a)
     if (which >= 0) next = token_at<VT>(w, which * seg, min(a.vocab, (which + 1) * seg), t, part);
     answer(a, n, w, next);
 }
-// Few queries: `chunks` workgroups sum a query's row, a piece per wavefront, and one wavefront, in a launch of its own, looks through the
-// piece that u falls into.  Bounded by two launches: 5 queries, 131072 tokens, 3.6 + 4.2 us.  (A workgroup there, with its barriers, took 8.8 us for a vocabulary of 131072.)
+// Long rows: `chunks` workgroups sum a query's row, a piece per wavefront, and one wavefront, in a launch of its own, looks through the
+// piece that u falls into.  Bounded by two launches where
+// queries are few (5, 131072 tokens: 3.6 + 4.2 us), by memory where they are many (320, 50021 tokens and draft probabilities: 16 + 7 us).  (A workgroup there, with its barriers, took 8.8 us for a vocabulary of 131072.)
 constexpr int CW = 4, CT = 64 * CW, kMostChunks = 64;
 __device__ __forceinline__ int piece_length(int vocab, int chunks) { return ((vocab + chunks * CW - 1) / (chunks * CW) + 3) / 4 * 4; }
 __global__ void __launch_bounds__(CT) verify_sum_kernel(const VerifyArgs a, double *sums)
@@ -595,9 +596,14 @@ __global__ void __launch_bounds__(64) verify_pick_kernel(const VerifyArgs a, con
     if (falls_into(v, std::false_type{})) next = lo + 8 * which_lane + which;
     answer(a, n, w, next);
 }
+// How many workgroups sum a query's row: 2048 in all where queries are few, one for every 8192 tokens where they are many, or compute units wait for the ones with
+// more work and for the tails of long rows (us with 1, and with 2, 3, 6, 12 a query: 320 queries of 50021 tokens 28.4, -, 25.9, 24.0, 24.5; 1100 65.8, -, 59.0, 54.0, 72.6;
+// 1500 of 20000 without draft probabilities 40.8, 28.4, -, 31.1, 37.0).
 int verify_chunks(int64_t n, int64_t vocab)
 {
-    return (int)std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(n, 1), (vocab + 2047) / 2048, (int64_t)kMostChunks}));
+    if (n > 65535) return 1;          // (queries are the grid's second axis)
+    const int64_t want = std::max(2048 / std::max<int64_t>(n, 1), (vocab + 4096) / 8192);
+    return (int)std::max<int64_t>(1, std::min<int64_t>({want, (vocab + 2047) / 2048, (int64_t)kMostChunks}));
 }
 
 }  // namespace
