@@ -333,8 +333,8 @@ __global__ void __launch_bounds__(256, 3) draft_own_kernel(const DraftArgs a)
 // Operands come straight from memory to registers: pages hold them in the order that v_mfma_f32_32x32x16 reads (S^T = K Q^T, O^T = V^T P^T: lane
 // (n, h) = (lane % 32, lane / 32) owns row n, as in the 128-row kernel).  The next unit's keys are asked for as soon as this one's
 // scores are formed, its values behind the second product.  Bounded by round trips: tile record, counts, rows, a unit each, the merge; past some units a
-// wavefront by what a compute unit takes in.  One query of 5 tokens, 8 KV heads, prompt of 411: 13.7 us (14.4 with 7 registers more of the new tokens'
-// operands held from the start); 5 queries over 3001 tokens in six ranges 20.6 us; two launches 20.8 and 30.3.
+// wavefront by what a compute unit takes in.  One query of 5 tokens, 8 KV heads, prompt of 411: 12.7 us (13.9 with the new tokens behind all cached units;
+// 13.6 with their lines fetched ahead into nothing, which the registers for it cost); 5 queries over 3001 tokens in six ranges 20.6 us; two launches 20.8 and 30.3.
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
@@ -407,8 +407,9 @@ __global__ void __launch_bounds__(FW * 64, 2) draft_few_kernel(const AttnArgs a)
         int src, base;               // FRESH: the pass's first row of the query; keys in its pages
         const char *p0, *p1;
     };
-    // The range's units: nc cached ones, then own ones from o0 on.
-    const int nc = (int)((int64_t)cached * (range + 1) / S) - key0 / 32;
+    // The range's units: nc cached ones and own ones from o0 on.  New tokens take longest (loaded, rotated, stored), so the last own unit, mostly one of
+    // those, is the last wavefront's first; the other wavefronts begin with cached ones.
+    const int nc = (int)((int64_t)cached * (range + 1) / S) - key0 / 32, c0 = min(nc, FW - 1);
     auto cached_unit = [&](int i, bool first) __attribute__((always_inline)) -> Unit {
         Unit x{};
         x.kind = CACHED;
@@ -464,7 +465,7 @@ __global__ void __launch_bounds__(FW * 64, 2) draft_few_kernel(const AttnArgs a)
     };
     // (cached keys need no counts: they travel while the rows are looked up)
     Unit x{};
-    if (wave < nc) {
+    if (wave < c0) {
         x = cached_unit(wave, true);
         load_keys(x);
         load_values(x);
@@ -492,9 +493,11 @@ __global__ void __launch_bounds__(FW * 64, 2) draft_few_kernel(const AttnArgs a)
     const int owns = __builtin_amdgcn_readlane(upto, 31), first_own = upto - units;
     const int o0 = (int)((int64_t)owns * range / S), u1 = nc + (int)((int64_t)owns * (range + 1) / S) - o0;
     auto unit_at = [&](int u) __attribute__((always_inline)) -> Unit {
-        if (u < nc) return cached_unit(u, false);
+        const bool any_own = u1 > nc;
+        if (u < c0 || !any_own) return cached_unit(u, false);
+        if (u > c0 && u <= nc) return cached_unit(u - 1, false);
         Unit x{};
-        const int w = o0 + u - nc;
+        const int w = o0 + (u == c0 ? u1 - nc : u - nc) - 1;
         const int L = __builtin_amdgcn_readfirstlane(63 - __builtin_clzll(__ballot(leads && first_own <= w)));
         const int old = __builtin_amdgcn_readlane(n_old, L), i = w - __builtin_amdgcn_readlane(first_own, L), pages = (old + kPageTokens - 1) / kPageTokens;
         x.sq = __builtin_amdgcn_readlane(row.sq, L);
@@ -514,7 +517,7 @@ __global__ void __launch_bounds__(FW * 64, 2) draft_few_kernel(const AttnArgs a)
         return x;
     };
     int u = wave;          // (wave-uniform, and so is the unit)
-    if (u >= nc && u < u1) {
+    if (u >= c0 && u < u1) {
         x = unit_at(u);
         load_keys(x);
         load_values(x);

@@ -715,7 +715,7 @@ void build_draft_tiles(sgc_plan *pl, int tile_rows)
     // One launch while its tiles' work, in rounds over 256 compute units of a fixed part (that of 20 units of 32 keys) and their units
     // (an own or new one counts as two cached ones: it is masked, and new keys are rotated), stays under 84 such units.  80 drawn
     // shapes: under it 0.55 to 0.97 times the two launches' time but for two (1.03, 1.10), above it 1.05 to 2.7 times but for two.
-    // 1 query of 5 tokens, 32 heads on 8, prompt of 411: 13.4 against 20.8 us; 10 prompts of 1024, 320 queries: 108 against 69 us.
+    // 1 query of 5 tokens, 32 heads on 8, prompt of 411: 12.7 against 20.8 us; 10 prompts of 1024, 320 queries: 108 against 69 us.
     // (ranges of 16 cached units, or of 24 units in all where queries have many of their own: 35 queries of 5 prompts of up to 267, up to 119 question tokens:
     // 22.8 us in one range, 19.4 in several)
     const int64_t ranges = std::max((2 * max_steps + 17) / 16, (2 * max_steps + 2 * own + 23) / 24);
