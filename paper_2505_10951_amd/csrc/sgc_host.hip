@@ -713,8 +713,8 @@ void build_draft_tiles(sgc_plan *pl, int tile_rows)
         }
     }
     // One launch while its tiles' work, in rounds over 256 compute units of a fixed part (that of 20 units of 32 keys) and their units
-    // (an own or new one counts as two cached ones: it is masked, and new keys are rotated), stays under 84 such units.  80 drawn
-    // shapes: under it 0.55 to 0.97 times the two launches' time but for two (1.03, 1.10), above it 1.05 to 2.7 times but for two.
+    // (an own or new one counts as two cached ones: it is masked, and new keys are rotated), stays under 84 such units.  104 shapes:
+    // where it is taken it has 0.58 to 0.97 times the two launches' time but for five (1.07 at most), elsewhere 1.03 to 3.0 times but for three (0.83 at least).
     // 1 query of 5 tokens, 32 heads on 8, prompt of 411: 12.7 against 20.8 us; 10 prompts of 1024, 320 queries: 108 against 69 us.
     // (ranges of 16 cached units, or of 24 units in all where queries have many of their own: 35 queries of 5 prompts of up to 267, up to 119 question tokens:
     // 22.8 us in one range, 19.4 in several)
