@@ -285,10 +285,11 @@ int probs_chunks(int64_t rows, int64_t vocab)
     const int64_t want = (512 + rows - 1) / std::max<int64_t>(rows, 1);
     return (int)std::max<int64_t>(1, std::min<int64_t>({want, (vocab + 4095) / 4096, 64}));
 }
-// Whether it is one, which reads the row once into registers: where the row fits, and is short or one of many.  us, one / several: 32-bit logits,
+// Whether it is one, which reads the row once into registers: where the row fits, and is short or one of many.  us on the GPU, one / several: 32-bit logits,
 // 1 x 8000 3.9 / 6.4, 20 x 16000 5.6 / 7.0, 20 x 32000 8.3 / 7.5, 40 x 32000 8.7 / 9.5, 40 x 50021 12.6 / 11.2, 80 x 50021 13.8 / 16.0,
 // 160 x 64000 23 / 32; 16 bits, 20 x 16000 5.8 / 6.6, 40 x 50021 15.3 / 11.9, 80 x 64000 16.6 / 18.3, 80 x 131072 36 / 31, 160 x 131072 44 / 46.
-bool probs_in_registers(int64_t rows, int64_t vocab, bool f32) { return row_vectors(vocab, f32) > 0 && (vocab <= 16384 || rows * 1000 >= vocab); }
+// A second launch costs the host 3 us, which a program that does not replay graphs waits for: 1 x 32000 8.0 / 10.6 with it, 1 x 40000 11.8 / 10.5.
+bool probs_in_registers(int64_t rows, int64_t vocab, bool f32) { return row_vectors(vocab, f32) > 0 && (vocab <= 8 * RT * 4 - 31 || rows * 1000 >= vocab); }
 template <typename T, int NV>
 void launch_rows(const T *x, int64_t xs, float *p, int64_t ps, int64_t rows, int vocab, float c, hipStream_t s)
 {

@@ -46,3 +46,12 @@ def test_first_of_equal_logits_wherever_the_row_begins():
             want = np.zeros(41, int)
             want[7] = vocab - 3
             assert np.array_equal(got.argmax(1), want) and np.array_equal(got.sum(1), np.ones(41))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab", [(3, 32736), (3, 32737), (3, 32738), (2, 24001)])
+def test_few_rows_at_the_second_launch(rows, vocab, dtype):
+    x = (torch.randn((rows, vocab), generator=torch.Generator().manual_seed(vocab)) * 3).to(TYPES[dtype][0])
+    x[0, vocab - 1] = 25.0
+    for T in (0.0, 0.7):
+        _check(x, T, 1, 2)
