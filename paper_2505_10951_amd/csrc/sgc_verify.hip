@@ -489,7 +489,7 @@ __device__ __forceinline__ void answer(const VerifyArgs &a, int64_t n, const Dra
 }
 
 // The draw goes down the row by sums in 64 bits, of parts that get smaller: the token is the first at which the running sum is beyond u times the whole.
-// Short rows: one workgroup a query.  8 wavefronts sum a segment each; the segment that u falls into is looked through token by token.
+// Short rows, and rows in front of which a launch is the larger part: one workgroup a query.  8 wavefronts sum a segment each; the segment that u falls into is looked through token by token.
 // Bounded by the chain of its sums (313 queries of 315 tokens 7.8 us).
 constexpr int VT = 512, VW = VT / 64;
 __global__ void __launch_bounds__(VT, 4) verify_kernel(const VerifyArgs a)
@@ -606,6 +606,10 @@ int verify_chunks(int64_t n, int64_t vocab)
     const int64_t want = std::max(2048 / std::max<int64_t>(n, 1), (vocab + 4096) / 8192);
     return (int)std::max<int64_t>(1, std::min<int64_t>({want, (vocab + 2047) / 2048, (int64_t)kMostChunks}));
 }
+// Whether it is one, in one launch: where there are few queries and what a workgroup reads of a row takes less than the second launch costs the host (us of
+// a program that does not replay graphs, one launch / two: 8 queries of 6000 tokens with draft probabilities 9.5 / 11.0, of 16000 10.9 / 11.1, of 32000 12.9 / 10.9, of 24000
+// without 10.3 / 11.1; 150 of 10000 with 11.0 / 11.0).
+bool verify_at_once(int64_t n, int64_t vocab, bool with_draft) { return n <= 256 && vocab * (with_draft ? 2 : 1) <= 24576; }
 
 }  // namespace
 
@@ -721,8 +725,8 @@ int sgc_verify_drafts(sgc_ctx *ctx, int32_t n_queries, int32_t max_rows, int32_t
     v.vocab = vocab;
     v.max_rows = max_rows;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    if (need > 0) {
-        const int chunks = verify_chunks(n_queries, vocab);
+    const int chunks = verify_at_once(n_queries, vocab, v.draft) ? 1 : verify_chunks(n_queries, vocab);
+    if (chunks > 1) {
         double *sums = static_cast<double *>(dev_workspace);
         hipLaunchKernelGGL(verify_sum_kernel, dim3((unsigned)chunks, (unsigned)n_queries), dim3(CT), 0, s, v, sums);
         hipLaunchKernelGGL(verify_pick_kernel, dim3((unsigned)n_queries), dim3(64), 0, s, v, sums, chunks);

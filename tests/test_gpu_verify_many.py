@@ -38,3 +38,8 @@ def test_drafts_that_cover_the_target_leave_its_own_row():
         tokens, u = rng.integers(0, V, size=(n, 2)), rng.random((n, 2)).astype(np.float32)
         rows, done = np.full(n, 2), np.zeros(n, int)
         _same(_verify(p, q, tokens, rows, u, done), _verify_ref(p, q, tokens, rows, u, done))
+
+
+@pytest.mark.parametrize("n,V,with_q", [(5, 12288, True), (5, 12289, True), (5, 24576, False), (5, 24577, False), (256, 9000, True), (257, 9000, True), (6, 40000, True)])
+def test_few_queries_at_the_second_launch(n, V, with_q):
+    test_verification(n, 2, V, with_q)
